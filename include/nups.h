@@ -353,6 +353,60 @@ nups_status nups_set_sync_period(nups_store* store, uint32_t period_us);
  * synchronises the stream.                                                    */
 nups_status nups_get_clip_stats(nups_store* store, double* h_sum, uint64_t* h_count, void* stream);
 
+/* ---- operators on model tensors -------------------------------------------- */
+/* What a model does around the rows that it pulls: normalise them, route items to
+ * experts whose parameters are keys, and shape the update of a row that holds a
+ * matrix before it is pushed.  Beyond pull_norm these calls do not touch the
+ * store's rows; the store gives them its device, its status word and its launch
+ * count.  Conventions:
+ *   - x_type and the like are NUPS_F32, NUPS_F64, NUPS_F16 or NUPS_BF16.
+ *   - Row i of a matrix argument starts `stride` VALUES after row i - 1 and its
+ *     values are contiguous; rows of an output must not overlap.  Any alignment
+ *     that suits the type is allowed, 16-byte aligned rows are fastest.
+ *   - Sums and statistics are held in fp32, or fp64 for fp64 values.
+ *   - d_scratch is the caller's device memory, 256-byte aligned, of at least the
+ *     bytes that the *_scratch call names for the same sizes; it needs no
+ *     initial value and holds nothing between calls.  Calls that may overlap on
+ *     the GPU (two streams, two captured graphs) need one each.
+ *   - Results do not depend on the order in which blocks run.
+ *   - Calls allocate nothing and may be captured into a CUDA graph.
+ *   - NUPS_ESTATE when the store's device is not current; NUPS_EINVAL for a type,
+ *     size, stride or pointer that is not allowed; n = 0 is allowed.             */
+enum { NUPS_F32 = 0, NUPS_F64 = 1, NUPS_F16 = 2, NUPS_BF16 = 3 };
+
+/* Layer norm of the n rows of x, `len` values each (1 <= len < 2^28):
+ *   mean = sum x / len, rstd = 1 / sqrt(sum (x - mean)^2 / len + eps),
+ *   y = (x - mean) rstd weight + bias.
+ * y has x's type; for fp32 x it may also be fp16 or bf16.  weight and bias (either
+ * may be NULL: 1 and 0) are of w_type: x's type or fp32 (fp64 x: fp64).  mean and
+ * rstd (NULL: not wanted) are fp32 (fp64 x: fp64), one value per row.  eps > 0.
+ * y may be x (same type and stride).                                           */
+nups_status nups_layer_norm(nups_store* store, const void* d_x, int x_type, uint64_t x_stride, uint64_t n, uint32_t len,
+                            const void* d_weight, const void* d_bias, int w_type, double eps, void* d_y, int y_type,
+                            uint64_t y_stride, void* d_mean, void* d_rstd, void* stream);
+
+/* pull, and layer norm of the pulled rows in the same pass: d_y[i][:] is the norm
+ * of what nups_pull gives for d_keys[i] (replica rows, access counts and keys out
+ * of range as there).  weight and bias have the store's value type, y_type as
+ * above.  d_rows (NULL: not wanted) receives the pulled rows themselves, which the
+ * backward pass reads.  d_y and d_rows are [n][value_len], 16-byte aligned.      */
+nups_status nups_pull_norm(nups_store* store, const uint32_t* d_keys, uint64_t n, const void* d_weight, const void* d_bias,
+                           double eps, void* d_y, int y_type, void* d_rows, void* d_mean, void* d_rstd, void* stream);
+
+/* The backward pass: from x, the statistics of the forward pass and dy (x's type;
+ * for fp32 x also fp16 or bf16), with h = (x - mean) rstd and g = dy weight,
+ *   dx = rstd (g - mean(g) - h mean(g h))      x's type, NULL: not wanted
+ *   dweight = sum over rows of dy h            w_type, NULL: not wanted
+ *   dbias = sum over rows of dy                w_type, NULL: not wanted
+ * The sums over rows run in an order fixed by n, len and the type.  With n = 0
+ * dweight and dbias are set to zero.  dx may be x or dy (same type and stride).
+ * Scratch is needed when dweight or dbias is wanted.                           */
+nups_status nups_layer_norm_grad(nups_store* store, const void* d_x, int x_type, uint64_t x_stride, const void* d_dy, int dy_type,
+                                 uint64_t dy_stride, uint64_t n, uint32_t len, const void* d_mean, const void* d_rstd,
+                                 const void* d_weight, int w_type, void* d_dx, uint64_t dx_stride, void* d_dweight, void* d_dbias,
+                                 void* d_scratch, uint64_t scratch_bytes, void* stream);
+nups_status nups_layer_norm_grad_scratch(nups_store* store, uint64_t n, uint32_t len, int x_type, uint64_t* h_bytes_out);
+
 /* ---- status and statistics ------------------------------------------------ */
 
 /* Read and clear the device status word (synchronises the stream): NUPS_OK,

@@ -19,6 +19,7 @@ OK, EINVAL, ENOMEM, ECUDA, EKEY, ESTATE, ETIMEOUT = 0, -1, -2, -3, -4, -5, -6
 SINGLE, REPLICATE = 0, 1
 CONFORM, BOUNDED, LONGTERM, NONCONFORM = 1, 2, 3, 4
 NOALLOC_MAX_ROWS = 65536
+TYPES = {torch.float32: 0, torch.float64: 1, torch.float16: 2, torch.bfloat16: 3}      # NUPS_F32 .. NUPS_BF16
 
 EXPORTS = [
     "nups_create", "nups_destroy", "nups_table_ptr", "nups_table_copy", "nups_init_uniform", "nups_pull", "nups_pull2", "nups_push",
@@ -29,6 +30,7 @@ EXPORTS = [
     "nups_shard_table_create", "nups_shard_table_destroy", "nups_shard_table_local", "nups_shard_table_copy", "nups_shard_table_export",
     "nups_shard_table_attach", "nups_shard_table_attach_ipc", "nups_shard_pull", "nups_shard_push", "nups_shard_status_check",
     "nups_shard_last_error", "nups_merge_mark", "nups_merge_export", "nups_merge_apply",
+    "nups_layer_norm", "nups_pull_norm", "nups_layer_norm_grad", "nups_layer_norm_grad_scratch",
 ]
 
 
@@ -114,6 +116,10 @@ def load(build_if_missing: bool = True):
         "nups_merge_mark": [vp, C.c_int, vp],
         "nups_merge_export": [vp, C.c_int, vp, vp],
         "nups_merge_apply": [vp, C.c_int, vp, vp, vp],
+        "nups_layer_norm": [vp, vp, C.c_int, u64, u64, u32, vp, vp, C.c_int, C.c_double, vp, C.c_int, u64, vp, vp, vp],
+        "nups_pull_norm": [vp, vp, u64, vp, vp, C.c_double, vp, C.c_int, vp, vp, vp, vp],
+        "nups_layer_norm_grad": [vp, vp, C.c_int, u64, vp, C.c_int, u64, u64, u32, vp, vp, vp, C.c_int, vp, u64, vp, vp, vp, u64, vp],
+        "nups_layer_norm_grad_scratch": [vp, u64, u32, C.c_int, C.POINTER(u64)],
     }
     for name, args in sig.items():
         fn = getattr(L, name)
@@ -150,6 +156,12 @@ def as_keys(t) -> torch.Tensor:
         t = t.to(torch.int64).cuda()
         t = torch.where(t >= 2 ** 31, t - 2 ** 32, t).to(torch.int32)
     return t.cuda().contiguous()
+
+
+def _type(t) -> int:
+    if t.dtype not in TYPES:
+        raise NupsError(EINVAL, "value type", f"{t.dtype} is none of {', '.join(map(str, TYPES))}")
+    return TYPES[t.dtype]
 
 
 class Store:
@@ -354,6 +366,94 @@ class Store:
         class _Raw:        # the library's buffer seen through the CUDA array interface, then copied out
             __cuda_array_interface__ = {"shape": (n.value,), "typestr": "<i4", "data": (p.value, False), "version": 2}
         return torch.as_tensor(_Raw(), device=self.device).clone()
+
+    # -- operators on model tensors -----------------------------------------------------
+    # All tensors are on the store's device, which is the current one; the calls run on its current stream.
+    def _on_device(self, what, *tensors):
+        if torch._C._cuda_getDevice() != self.device.index:
+            raise NupsError(ESTATE, what, f"the store is on {self.device}, which is not the current device")
+        for t in tensors:
+            if t is not None and t.device != self.device:
+                raise NupsError(EINVAL, what, f"a tensor is on {t.device}, the store on {self.device}")
+
+    def _rows(self, what, t, n=None, length=None):
+        """(address, stride) of a matrix whose rows are contiguous; rows may lie apart from one another."""
+        if t.dim() != 2 or (n is not None and tuple(t.shape) != (n, length)):
+            raise NupsError(EINVAL, what, f"expected a matrix{'' if n is None else f' of {n} x {length}'}, got {tuple(t.shape)}")
+        if t.shape[1] > 1 and t.stride(1) != 1:
+            raise NupsError(EINVAL, what, "the values of a row must be contiguous")
+        stride = t.stride(0) if t.shape[0] > 1 else t.shape[1]
+        if stride < t.shape[1]:
+            raise NupsError(EINVAL, what, "rows must not overlap")
+        return t.data_ptr(), stride
+
+    def _vector(self, what, t, length, dtype=None):
+        if t is None:
+            return None
+        if tuple(t.shape) != (length,) or (length > 1 and t.stride(0) != 1) or (dtype is not None and t.dtype != dtype):
+            raise NupsError(EINVAL, what, f"expected {length} contiguous values{'' if dtype is None else f' of {dtype}'}, got {tuple(t.shape)} of {t.dtype}")
+        return t.data_ptr()
+
+    def _params(self, what, x_dtype, length, *vectors):
+        """Type of the parameters given (x's type, or float32), and their addresses."""
+        given = [v for v in vectors if v is not None]
+        dtype = given[0].dtype if given else x_dtype
+        if any(v.dtype != dtype for v in given):
+            raise NupsError(EINVAL, what, "weight and bias must be of one type")
+        return dtype, [self._vector(what, v, length) for v in vectors]
+
+    def layer_norm(self, x, weight=None, bias=None, eps=1e-5, out_dtype=None, stats=True, out=None):
+        """(y, mean, rstd) of the rows of x [n, len]; stats=False: y alone.  out may be x itself."""
+        w = "nups_layer_norm"
+        if out is None:
+            out = torch.empty(x.shape, dtype=out_dtype or x.dtype, device=x.device)
+        self._on_device(w, x, weight, bias, out)
+        (px, xs), (py, ys) = self._rows(w, x), self._rows(w, out, *x.shape)
+        n, length = x.shape
+        dtype, (pw, pb) = self._params(w, x.dtype, length, weight, bias)
+        keep = torch.float64 if x.dtype == torch.float64 else torch.float32
+        mean, rstd = (torch.empty(n, dtype=keep, device=x.device) for _ in range(2)) if stats else (None, None)
+        self._chk(self._l.nups_layer_norm(self._s, px, _type(x), xs, n, length, pw, pb, TYPES.get(dtype, -1), eps, py, _type(out), ys,
+                                          _ptr(mean), _ptr(rstd), _stream()), w)
+        return (out, mean, rstd) if stats else out
+
+    def pull_norm(self, keys, weight=None, bias=None, eps=1e-5, out_dtype=None, stats=True, rows=False):
+        """Layer norm of the pulled rows: (y, mean, rstd), and with rows=True also the rows; stats=False: without mean and rstd."""
+        w, n = "nups_pull_norm", keys.numel()
+        self._on_device(w, keys, weight, bias)
+        dtype, (pw, pb) = self._params(w, self.dtype, self.L, weight, bias)
+        if dtype != self.dtype:
+            raise NupsError(EINVAL, w, f"weight and bias must be of the store's type, {self.dtype}")
+        y = torch.empty((n, self.L), dtype=out_dtype or self.dtype, device=self.device)
+        pulled = torch.empty((n, self.L), dtype=self.dtype, device=self.device) if rows else None
+        mean, rstd = (torch.empty(n, dtype=self.dtype, device=self.device) for _ in range(2)) if stats else (None, None)
+        self._chk(self._l.nups_pull_norm(self._s, _ptr(keys, torch.int32), n, pw, pb, eps, _ptr(y), _type(y), _ptr(pulled), _ptr(mean),
+                                         _ptr(rstd), _stream()), w)
+        res = (y, mean, rstd) if stats else (y,)
+        res = res + (pulled,) if rows else res
+        return res if len(res) > 1 else y
+
+    def layer_norm_grad(self, x, dy, mean, rstd, weight=None, need_dx=True, need_params=True, dx=None):
+        """(dx, dweight, dbias) of layer_norm; what is not needed is None.  dweight and dbias have weight's type (x's without one)."""
+        w = "nups_layer_norm_grad"
+        n, length = x.shape if x.dim() == 2 else (0, 0)
+        if need_dx and dx is None:
+            dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        self._on_device(w, x, dy, mean, rstd, weight, dx)
+        (px, xs), (pdy, dys) = self._rows(w, x), self._rows(w, dy, n, length)
+        pdx, dxs = self._rows(w, dx, n, length) if dx is not None else (None, length)
+        if dx is not None and dx.dtype != x.dtype:
+            raise NupsError(EINVAL, w, "dx must have x's type")
+        keep = torch.float64 if x.dtype == torch.float64 else torch.float32
+        pm, pr = self._vector(w, mean, n, keep), self._vector(w, rstd, n, keep)
+        dtype, (pw,) = self._params(w, x.dtype, length, weight)
+        dweight, dbias = (torch.empty(length, dtype=dtype, device=x.device) for _ in range(2)) if need_params else (None, None)
+        size = C.c_uint64()
+        self._chk(self._l.nups_layer_norm_grad_scratch(self._s, n, length, _type(x), C.byref(size)), w)
+        scratch = torch.empty(size.value, dtype=torch.uint8, device=x.device)
+        self._chk(self._l.nups_layer_norm_grad(self._s, px, _type(x), xs, pdy, _type(dy), dys, n, length, pm, pr, pw, TYPES.get(dtype, -1), pdx, dxs,
+                                               _ptr(dweight), _ptr(dbias), _ptr(scratch), size.value, _stream()), w)
+        return dx, dweight, dbias
 
     # -- status -------------------------------------------------------------------------
     def status_check(self):
