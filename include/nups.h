@@ -407,6 +407,43 @@ nups_status nups_layer_norm_grad(nups_store* store, const void* d_x, int x_type,
                                  void* d_scratch, uint64_t scratch_bytes, void* stream);
 nups_status nups_layer_norm_grad_scratch(nups_store* store, uint64_t n, uint32_t len, int x_type, uint64_t* h_bytes_out);
 
+/* A router over `experts` keys: softmax and choice of the `top` largest logits of
+ * each of n items, how often every expert was chosen, and the losses that keep the
+ * choices even.  With p = softmax of an item's logits, T = number of items that
+ * take part, counts[e] = how many of them chose e:
+ *   d_choice[i][j]  the j-th largest logit's expert (the lower number among equals)
+ *   d_weight[i][j]  its p; with renormalize = 1 divided by the item's sum of them
+ *   d_lse[i]        log of the sum of the exponentials (NULL: not wanted)
+ *   d_prob[e]       P_e = sum of p_e over the items / T (NULL: not wanted)
+ *   d_loss[0..2]    balance * B + z * Z, B, Z (NULL: not wanted) with
+ *                   B = experts / (top T) * sum_e counts[e] P_e, Z = sum lse^2 / T
+ *   d_counts[e], *d_tokens = T
+ * d_active (NULL: all) is one byte per item: 0 = the item takes no part, whatever its
+ * logits hold; its choices are -1 and its other results 0.  So are those of an item
+ * whose logits are all -infinity.  A logit of -infinity is not chosen (-1 and 0
+ * where fewer than `top` are left), and neither is NaN.  NaN and +infinity make the
+ * item's p, and with it prob and the losses, NaN.  T = 0: prob and loss are 0.  Choices are keys as the store's
+ * calls take them where experts are its first keys.  type is NUPS_F32, NUPS_F16 or
+ * NUPS_BF16; 1 <= experts <= NUPS_ROUTE_MAX_EXPERTS; top <= experts,
+ * NUPS_ROUTE_MAX_TOP.                                                           */
+#define NUPS_ROUTE_MAX_EXPERTS 1024
+#define NUPS_ROUTE_MAX_TOP 32
+nups_status nups_route(nups_store* store, const void* d_logits, int type, uint64_t stride, uint64_t n, uint32_t experts, uint32_t top,
+                       const uint8_t* d_active, int renormalize, float balance, float z, int32_t* d_choice, float* d_weight,
+                       float* d_lse, uint64_t* d_counts, uint64_t* d_tokens, float* d_prob, float* d_loss, void* d_scratch,
+                       uint64_t scratch_bytes, void* stream);
+nups_status nups_route_scratch(nups_store* store, uint64_t n, uint32_t experts, uint64_t* h_bytes_out);
+
+/* The gradient of the logits from that of the loss (d_dloss, one float; NULL: 1)
+ * and that of the weights (d_dweight [n][top]; NULL: 0).  Choices and counts are
+ * constants.  d_choice, d_lse, d_counts and d_tokens are what nups_route gave for the
+ * same arguments.  d_dlogits has the logits' type; items that took no part get 0.
+ * d_dlogits may be d_logits (same stride).                                      */
+nups_status nups_route_grad(nups_store* store, const void* d_logits, int type, uint64_t stride, uint64_t n, uint32_t experts, uint32_t top,
+                            const uint8_t* d_active, int renormalize, float balance, float z, const int32_t* d_choice,
+                            const float* d_lse, const uint64_t* d_counts, const uint64_t* d_tokens, const float* d_dloss,
+                            const float* d_dweight, void* d_dlogits, uint64_t dlogits_stride, void* stream);
+
 /* ---- status and statistics ------------------------------------------------ */
 
 /* Read and clear the device status word (synchronises the stream): NUPS_OK,

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -31,6 +32,7 @@ EXPORTS = [
     "nups_shard_table_attach", "nups_shard_table_attach_ipc", "nups_shard_pull", "nups_shard_push", "nups_shard_status_check",
     "nups_shard_last_error", "nups_merge_mark", "nups_merge_export", "nups_merge_apply",
     "nups_layer_norm", "nups_pull_norm", "nups_layer_norm_grad", "nups_layer_norm_grad_scratch",
+    "nups_route", "nups_route_scratch", "nups_route_grad",
 ]
 
 
@@ -120,6 +122,9 @@ def load(build_if_missing: bool = True):
         "nups_pull_norm": [vp, vp, u64, vp, vp, C.c_double, vp, C.c_int, vp, vp, vp, vp],
         "nups_layer_norm_grad": [vp, vp, C.c_int, u64, vp, C.c_int, u64, u64, u32, vp, vp, vp, C.c_int, vp, u64, vp, vp, vp, u64, vp],
         "nups_layer_norm_grad_scratch": [vp, u64, u32, C.c_int, C.POINTER(u64)],
+        "nups_route": [vp, vp, C.c_int, u64, u64, u32, u32, vp, C.c_int, f32, f32, vp, vp, vp, vp, vp, vp, vp, vp, u64, vp],
+        "nups_route_scratch": [vp, u64, u32, C.POINTER(u64)],
+        "nups_route_grad": [vp, vp, C.c_int, u64, u64, u32, u32, vp, C.c_int, f32, f32, vp, vp, vp, vp, vp, vp, vp, u64, vp],
     }
     for name, args in sig.items():
         fn = getattr(L, name)
@@ -162,6 +167,21 @@ def _type(t) -> int:
     if t.dtype not in TYPES:
         raise NupsError(EINVAL, "value type", f"{t.dtype} is none of {', '.join(map(str, TYPES))}")
     return TYPES[t.dtype]
+
+
+class Routing(NamedTuple):
+    """What Store.route gives, and the settings that Store.route_grad needs again."""
+    choice: torch.Tensor                # [n, top] int32, -1 = none
+    weight: torch.Tensor                # [n, top]
+    counts: torch.Tensor                # [experts] int64
+    tokens: torch.Tensor                # int64, items that took part
+    prob: Optional[torch.Tensor]        # [experts]
+    loss: Optional[torch.Tensor]        # [3]: weighted sum, balance loss, z loss
+    lse: Optional[torch.Tensor]         # [n]
+    active: Optional[torch.Tensor]
+    renormalize: bool
+    balance: float
+    z: float
 
 
 class Store:
@@ -454,6 +474,56 @@ class Store:
         self._chk(self._l.nups_layer_norm_grad(self._s, px, _type(x), xs, pdy, _type(dy), dys, n, length, pm, pr, pw, TYPES.get(dtype, -1), pdx, dxs,
                                                _ptr(dweight), _ptr(dbias), _ptr(scratch), size.value, _stream()), w)
         return dx, dweight, dbias
+
+    def _active(self, what, active, n):
+        if active is None:
+            return None
+        if active.dtype not in (torch.bool, torch.uint8):
+            raise NupsError(EINVAL, what, f"active must be bool or uint8, got {active.dtype}")
+        return self._vector(what, active, n)
+
+    def route(self, logits, top, active=None, renormalize=False, balance=0.0, z=0.0, losses=True):
+        """Softmax over experts and choice of the `top` largest of every item; see Routing.  losses=False (a program that only
+        answers): without prob, loss and lse."""
+        w = "nups_route"
+        self._on_device(w, logits, active)
+        p, stride = self._rows(w, logits)
+        n, experts = logits.shape
+        pa = self._active(w, active, n)
+        dev = logits.device
+        choice = torch.empty((n, top), dtype=torch.int32, device=dev)
+        weight = torch.empty((n, top), dtype=torch.float32, device=dev)
+        counts, tokens = torch.empty(experts, dtype=torch.int64, device=dev), torch.empty((), dtype=torch.int64, device=dev)
+        prob, loss, lse = (torch.empty(k, dtype=torch.float32, device=dev) for k in (experts, 3, n)) if losses else (None, None, None)
+        size = C.c_uint64()
+        self._chk(self._l.nups_route_scratch(self._s, n, experts, C.byref(size)), w)
+        scratch = torch.empty(size.value, dtype=torch.uint8, device=dev)
+        self._chk(self._l.nups_route(self._s, p, _type(logits), stride, n, experts, top, pa, int(renormalize), balance, z, _ptr(choice), _ptr(weight),
+                                     _ptr(lse), _ptr(counts), _ptr(tokens), _ptr(prob), _ptr(loss), _ptr(scratch), size.value, _stream()), w)
+        return Routing(choice, weight, counts, tokens, prob, loss, lse, active, renormalize, balance, z)
+
+    def route_grad(self, logits, routing, dweight=None, dloss=None, out=None):
+        """Gradient of the logits from those of the weights [n, top] and of loss[0] (one value; None: 1).  `routing` is what
+        route gave for these logits; its counts and tokens may have been added up over several processes."""
+        w, r = "nups_route_grad", routing
+        if r.lse is None:
+            raise NupsError(EINVAL, w, "the forward call was made with losses=False")
+        out = torch.empty_like(logits, memory_format=torch.contiguous_format) if out is None else out
+        self._on_device(w, logits, r.choice, r.active, dweight, dloss, out)
+        p, stride = self._rows(w, logits)
+        n, experts = logits.shape
+        po, os_ = self._rows(w, out, n, experts)
+        top = r.choice.shape[1]
+        if out.dtype != logits.dtype or tuple(r.choice.shape) != (n, top) or r.counts.numel() != experts:
+            raise NupsError(EINVAL, w, "out must have the logits' type, and the routing must be of these logits")
+        if dweight is not None and (tuple(dweight.shape) != (n, top) or dweight.dtype != torch.float32 or not dweight.is_contiguous()):
+            raise NupsError(EINVAL, w, f"dweight must be a contiguous float32 {n} x {top}")
+        if dloss is not None and (dloss.numel() != 1 or dloss.dtype != torch.float32):
+            raise NupsError(EINVAL, w, "dloss must be one float32")
+        self._chk(self._l.nups_route_grad(self._s, p, _type(logits), stride, n, experts, top, self._active(w, r.active, n), int(r.renormalize), r.balance,
+                                          r.z, _ptr(r.choice), self._vector(w, r.lse, n), _ptr(r.counts, torch.int64), _ptr(r.tokens, torch.int64),
+                                          _ptr(dloss), _ptr(dweight), po, os_, _stream()), w)
+        return out
 
     # -- status -------------------------------------------------------------------------
     def status_check(self):

@@ -1,0 +1,589 @@
+// A router over experts: softmax and choice of the largest logits per item, counts per expert, balance and z losses, and the
+// gradient of the logits.
+//
+// One pass over the logits per direction.  An item's logits are held in the registers of a team of TPR lanes (EPT each).  The
+// choice takes one reduction over the team per chosen expert: each lane keeps its two largest logits as whole numbers in the
+// order of the logits (for 16-bit types with the expert's number in the bits that the logit leaves free, so that equal logits
+// are told apart by the same comparison), and looks through its logits again only when both were chosen.  The sums over items
+// (P, lse^2) stay in registers until the block ends; blocks leave them in scratch and a last small kernel adds them in order.
+#include <cooperative_groups.h>
+#include <math.h>
+#include <math_constants.h>
+
+#include "nups_types.cuh"
+
+namespace {
+
+struct RouteArgs {
+    const void* logits;
+    uint64_t stride, n;
+    uint32_t experts, top;
+    const uint8_t* active;
+    int renormalize, sums;     // sums: P and Z are wanted
+    float balance, z;
+    int32_t* choice;
+    float *weight, *lse;
+    uint64_t *counts, *tokens;
+    float *prob, *loss;
+    float* part_p;             // [blocks][experts], then [blocks] sums of lse^2
+    uint32_t* part_c;          // [blocks][experts] counts, then [blocks] items
+};
+
+constexpr int ROUTE_BLOCK = 256;
+__host__ __device__ constexpr int route_slots(int tpr) { return tpr == 32 ? 1 : 4; }      // chosen experts that a lane keeps
+
+template <int TPR> __device__ __forceinline__ float lanes_sum(float x)
+{
+#pragma unroll
+    for (int o = TPR / 2; o > 0; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
+    return x;
+}
+template <int TPR> __device__ __forceinline__ uint32_t lanes_max(uint32_t x)
+{
+    if constexpr (TPR == 32) {
+        return __reduce_max_sync(0xFFFFFFFFu, x);
+    } else {
+#pragma unroll
+        for (int o = TPR / 2; o > 0; o >>= 1) x = max(x, __shfl_xor_sync(0xFFFFFFFFu, x, o));
+        return x;
+    }
+}
+template <int TPR> __device__ __forceinline__ uint32_t lanes_min(uint32_t x)
+{
+    if constexpr (TPR == 32) {
+        return __reduce_min_sync(0xFFFFFFFFu, x);
+    } else {
+#pragma unroll
+        for (int o = TPR / 2; o > 0; o >>= 1) x = min(x, __shfl_xor_sync(0xFFFFFFFFu, x, o));
+        return x;
+    }
+}
+
+// Whole numbers in the order of the logits; 0 = never chosen (-infinity, NaN).  -0 counts as +0.
+__device__ __forceinline__ uint32_t ordered(float x)
+{
+    const uint32_t b = __float_as_uint(x + 0.0f);
+    return x > -CUDART_INF_F ? b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u) : 0u;
+}
+__device__ __forceinline__ float from_ordered(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u); }
+// fp16 and bf16 leave at least 13 bits of a float's mantissa free: the larger number there is the lower expert
+constexpr uint32_t FREE = 0x1FFFu;
+__device__ __forceinline__ uint32_t ordered_with(float x, uint32_t e)
+{
+    const uint32_t u = ordered(x);
+    return u ? (u & ~FREE) | (FREE - e) : 0u;
+}
+__device__ __forceinline__ float logit_of(uint32_t key) { return from_ordered(key & 0x80000000u ? key & ~FREE : key | FREE); }
+
+template <int TPR, int VEC> __device__ __forceinline__ uint32_t expert_at(int i, int t)
+{
+    return (uint32_t)(((i / VEC) * TPR + t) * VEC + i % VEC);
+}
+
+template <class X, int VEC, int TPR, int EPT>
+__device__ __forceinline__ void load_logits(const X* row, bool in, uint32_t experts, int t, float fill, float (&x)[EPT])
+{
+#pragma unroll
+    for (int c = 0; c < EPT / VEC; ++c) {
+        const uint32_t e = expert_at<TPR, VEC>(c * VEC, t);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) x[c * VEC + j] = fill;
+        if (in && e < experts) unpack<float>(load_pack<X, VEC>(row + e), x + c * VEC);
+    }
+}
+
+// Counts and mean of one expert; returns its share of B's sum.
+__device__ __forceinline__ float finish_expert(const RouteArgs& a, uint32_t e, float p, uint32_t c, float T)
+{
+    const float P = p / T;
+    a.counts[e] = c;
+    if (a.prob) a.prob[e] = P;
+    return (float)c * P;
+}
+// What is left when B's sum is known; one thread.
+__device__ __forceinline__ void finish_losses(const RouteArgs& a, float b, float z, uint32_t tokens, float T)
+{
+    *a.tokens = tokens;
+    if (!a.loss) return;
+    const float B = b * ((float)a.experts / ((float)a.top * T)), Z = z / T;
+    a.loss[0] = a.balance * B + a.z * Z;
+    a.loss[1] = B;
+    a.loss[2] = Z;
+}
+
+template <class X, int VEC, int TPR, int EPT>
+__global__ void __launch_bounds__(ROUTE_BLOCK) route_kernel(RouteArgs a)
+{
+    constexpr int TEAMS = ROUTE_BLOCK / TPR, CAP = TPR * EPT, SLOTS = route_slots(TPR), WARPS = ROUTE_BLOCK / 32;
+    constexpr bool PACKED = sizeof(X) == 2;
+    __shared__ uint32_t chosen[CAP];                        // counts of this block
+    __shared__ float sums[WARPS][CAP > 512 ? 512 : CAP];
+    __shared__ float zsum[WARPS];
+    __shared__ uint32_t tsum[WARPS];
+    for (int e = threadIdx.x; e < CAP; e += ROUTE_BLOCK) chosen[e] = 0;
+    __syncthreads();
+    grid_dependency_wait();
+    const int t = threadIdx.x % TPR, team = threadIdx.x / TPR;
+    float acc[EPT], zacc = 0;
+    uint32_t items = 0;
+#pragma unroll
+    for (int i = 0; i < EPT; ++i) acc[i] = 0;
+    for (uint64_t base = (uint64_t)blockIdx.x * TEAMS; base < a.n; base += (uint64_t)gridDim.x * TEAMS) {
+        const uint64_t row = base + team;
+        const bool in = row < a.n;
+        bool on = in && (!a.active || a.active[row]);
+        float x[EPT];
+        load_logits<X, VEC, TPR, EPT>((const X*)a.logits + row * a.stride, on, a.experts, t, -CUDART_INF_F, x);
+        // the lane's two largest
+        uint32_t first = 0, second = 0, e_first = 0;
+#pragma unroll
+        for (int i = 0; i < EPT; ++i) {
+            const uint32_t e = expert_at<TPR, VEC>(i, t);
+            const uint32_t u = PACKED ? ordered_with(x[i], e) : ordered(x[i]);
+            if (PACKED) second = max(second, min(first, u));
+            if (u > first) { first = u; e_first = e; }
+        }
+        uint32_t slot_u[SLOTS];
+        int32_t slot_e[SLOTS];
+        float most = 0;
+        bool any = false;
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s) {
+            slot_u[s] = 0;
+            slot_e[s] = -1;
+            if (s * TPR >= (int)a.top) continue;
+            for (int l = 0; l < TPR; ++l) {
+                if (s * TPR + l >= (int)a.top) break;
+                const uint32_t u = lanes_max<TPR>(first);
+                uint32_t e;
+                if (PACKED) {
+                    e = FREE - (u & FREE);
+                    if (first == u) {
+                        first = second;
+                        second = 0;
+                        if (first == 0) {                   // both were chosen: look for the next two among all
+#pragma unroll
+                            for (int i = 0; i < EPT; ++i) {
+                                const uint32_t w = ordered_with(x[i], expert_at<TPR, VEC>(i, t));
+                                const uint32_t below = w < u ? w : 0u;
+                                second = max(second, min(first, below));
+                                first = max(first, below);
+                            }
+                        }
+                    }
+                } else {
+                    e = lanes_min<TPR>(first == u ? e_first : 0xFFFFFFFFu);
+                    if (first == u && e_first == e && u) {  // the lane's next: smaller, or equal and further on
+                        uint32_t next = 0, e_next = 0;
+#pragma unroll
+                        for (int i = 0; i < EPT; ++i) {
+                            const uint32_t w = ordered(x[i]), ei = expert_at<TPR, VEC>(i, t);
+                            if ((w < u || (w == u && ei > e)) && w > next) { next = w; e_next = ei; }
+                        }
+                        first = next;
+                        e_first = e_next;
+                    }
+                }
+                if (s == 0 && l == 0) {
+                    any = u != 0;
+                    most = any ? (PACKED ? logit_of(u) : from_ordered(u)) : 0.0f;
+                }
+                if (t == l && u) { slot_u[s] = u; slot_e[s] = (int32_t)e; }
+            }
+        }
+        float ex[EPT], total = 0;
+#pragma unroll
+        for (int i = 0; i < EPT; ++i) {
+            ex[i] = __expf(x[i] - most);
+            total += ex[i];
+        }
+        total = lanes_sum<TPR>(total);
+        if (!any && total == 0.0f) on = false;              // nothing but -infinity
+        const float inv = on ? 1.0f / total : 0.0f;
+        float kept[SLOTS], kept_sum = 0;
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s) {
+            kept[s] = slot_e[s] >= 0 ? __expf((PACKED ? logit_of(slot_u[s]) : from_ordered(slot_u[s])) - most) : 0.0f;
+            kept_sum += kept[s];
+        }
+        float scale = inv;
+        if (a.renormalize) {
+            kept_sum = lanes_sum<TPR>(kept_sum);
+            scale = kept_sum != 0.0f ? 1.0f / kept_sum : 0.0f;
+        }
+        if (in) {
+#pragma unroll
+            for (int s = 0; s < SLOTS; ++s) {
+                const uint32_t j = s * TPR + t;
+                if (j < a.top) {
+                    a.choice[row * a.top + j] = slot_e[s];
+                    a.weight[row * a.top + j] = slot_e[s] >= 0 ? kept[s] * scale : 0.0f;
+                    if (slot_e[s] >= 0) atomicAdd(&chosen[slot_e[s]], 1u);
+                }
+            }
+        }
+        if (on) {
+            const float lse = most + logf(total);
+            if (t == 0) {
+                if (a.lse) a.lse[row] = lse;
+                zacc += lse * lse;
+                ++items;
+            }
+            if (a.sums)
+#pragma unroll
+                for (int i = 0; i < EPT; ++i) acc[i] += ex[i] * inv;
+        } else if (in && t == 0 && a.lse) {
+            a.lse[row] = 0.0f;
+        }
+    }
+    // the block's sums: teams of a warp by shuffles, warps through shared memory
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+#pragma unroll
+    for (int o = 16; o >= TPR; o >>= 1)
+#pragma unroll
+        for (int i = 0; i < EPT; ++i) acc[i] += __shfl_xor_sync(0xFFFFFFFFu, acc[i], o);
+    zacc = lanes_sum<32>(zacc);
+    items = __reduce_add_sync(0xFFFFFFFFu, items);
+    if (lane == 0) { zsum[warp] = zacc; tsum[warp] = items; }
+    __syncthreads();
+    float z = 0;
+    uint32_t m = 0;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) { z += zsum[w]; m += tsum[w]; }
+    const bool alone = gridDim.x == 1;                      // this block's sums are the call's
+    const float T = m ? (float)m : 1.0f;
+    constexpr int PART = CAP > 512 ? 512 : CAP;             // experts per round
+    float b = 0;
+#pragma unroll
+    for (int r = 0; r < CAP / PART; ++r) {
+        __syncthreads();
+        if (lane < TPR)
+#pragma unroll
+            for (int i = 0; i < EPT; ++i) {
+                const uint32_t e = expert_at<TPR, VEC>(i, t);
+                if (e / PART == r) sums[warp][e % PART] = acc[i];
+            }
+        __syncthreads();
+        for (int k = threadIdx.x; k < PART; k += ROUTE_BLOCK) {
+            const uint32_t e = r * PART + k;
+            float p = 0;
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) p += sums[w][k];
+            if (e < a.experts) {
+                if (alone) {
+                    b += finish_expert(a, e, p, chosen[e], T);
+                } else {
+                    a.part_p[(uint64_t)blockIdx.x * a.experts + e] = p;
+                    a.part_c[(uint64_t)blockIdx.x * a.experts + e] = chosen[e];
+                }
+            }
+        }
+    }
+    if (alone) {
+        b = lanes_sum<32>(b);
+        __syncthreads();
+        if (lane == 0) zsum[warp] = b;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            b = 0;
+            for (int w = 0; w < WARPS; ++w) b += zsum[w];
+            finish_losses(a, b, z, m, T);
+        }
+    } else if (threadIdx.x == 0) {
+        a.part_p[(uint64_t)gridDim.x * a.experts + blockIdx.x] = z;
+        a.part_c[(uint64_t)gridDim.x * a.experts + blockIdx.x] = m;
+    }
+}
+
+constexpr int JOIN_BLOCK = 1024, JOIN_CLUSTER = 8;
+// The sums of all blocks: a cluster whose blocks take `width` experts each, JOIN_BLOCK / width threads per expert.
+__global__ void __cluster_dims__(JOIN_CLUSTER) __launch_bounds__(JOIN_BLOCK) route_join_kernel(RouteArgs a, uint32_t blocks, uint32_t width)
+{
+    __shared__ float sp[JOIN_BLOCK];
+    __shared__ uint32_t sc[JOIN_BLOCK];
+    __shared__ float shared[32];
+    __shared__ uint32_t shared_t[32];
+    __shared__ float share;                                 // this block's part of B's sum
+    grid_dependency_wait();
+    const uint32_t run = threadIdx.x / width, runs = JOIN_BLOCK / width, e = blockIdx.x * width + threadIdx.x % width;
+    float p = 0;
+    uint32_t c = 0;
+    if (e < a.experts)
+#pragma unroll 8
+        for (uint32_t b = run; b < blocks; b += runs) {
+            p += __ldcg(a.part_p + (uint64_t)b * a.experts + e);
+            c += __ldcg(a.part_c + (uint64_t)b * a.experts + e);
+        }
+    float z = 0;
+    uint32_t m = 0;
+    for (uint32_t b = threadIdx.x; b < blocks; b += JOIN_BLOCK) {
+        z += __ldcg(a.part_p + (uint64_t)blocks * a.experts + b);
+        m += __ldcg(a.part_c + (uint64_t)blocks * a.experts + b);
+    }
+    z = lanes_sum<32>(z);
+    m = __reduce_add_sync(0xFFFFFFFFu, m);
+    if ((threadIdx.x & 31) == 0) { shared[threadIdx.x >> 5] = z; shared_t[threadIdx.x >> 5] = m; }
+    sp[threadIdx.x] = p;
+    sc[threadIdx.x] = c;
+    __syncthreads();
+    z = lanes_sum<32>(shared[threadIdx.x & 31]);
+    m = __reduce_add_sync(0xFFFFFFFFu, shared_t[threadIdx.x & 31]);
+    for (uint32_t half = runs / 2; half > 0; half /= 2) {   // a tree over the runs
+        if (run < half) {
+            sp[threadIdx.x] += sp[threadIdx.x + half * width];
+            sc[threadIdx.x] += sc[threadIdx.x + half * width];
+        }
+        __syncthreads();
+    }
+    const float T = m ? (float)m : 1.0f;
+    float b = run == 0 && e < a.experts ? finish_expert(a, e, sp[threadIdx.x], sc[threadIdx.x], T) : 0.0f;
+    b = lanes_sum<32>(b);
+    if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = b;
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        b = lanes_sum<32>(shared[threadIdx.x]);
+        if (threadIdx.x == 0) share = b;
+    }
+    cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
+    cluster.sync();
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        b = 0;
+        for (unsigned r = 0; r < JOIN_CLUSTER; ++r) b += *cluster.map_shared_rank(&share, r);
+        finish_losses(a, b, z, m, T);
+    }
+    cluster.sync();                                         // the blocks' shared memory stays until it was read
+}
+
+struct RouteGradArgs {
+    const void* logits;
+    uint64_t stride, n;
+    uint32_t experts, top;
+    const uint8_t* active;
+    int renormalize;
+    float balance, z;
+    const int32_t* choice;
+    const float* lse;
+    const uint64_t *counts, *tokens;
+    const float *dloss, *dweight;
+    void* dlogits;
+    uint64_t dstride;
+};
+
+// d_e = p_e (g_e - sum g p + 2 z dloss lse / T), g_e = balance dloss f_e / T (+ dweight where e was chosen); with renormalized
+// weights the choices add w (dweight - sum dweight w) instead.  What the choices add is left in the team's row of shared memory
+// by the lanes that hold them and picked up by the lanes that hold the logits.
+template <class X, int VEC, int TPR, int EPT>
+__global__ void __launch_bounds__(ROUTE_BLOCK) route_grad_kernel(RouteGradArgs a)
+{
+    constexpr int TEAMS = ROUTE_BLOCK / TPR, CAP = TPR * EPT, SLOTS = route_slots(TPR);
+    __shared__ float extra[TEAMS][CAP];
+    const int t = threadIdx.x % TPR, team = threadIdx.x / TPR;
+    for (int e = t; e < CAP; e += TPR) extra[team][e] = 0.0f;
+    grid_dependency_wait();
+    const uint64_t tokens = *a.tokens;
+    const float T = tokens ? (float)tokens : 1.0f;
+    const float dloss = a.dloss ? *a.dloss : 1.0f;
+    const float zf = dloss * a.z * 2.0f / T, bf = dloss * a.balance / T * ((float)a.experts / ((float)a.top * T));
+    float g[EPT];
+#pragma unroll
+    for (int i = 0; i < EPT; ++i) {
+        const uint32_t e = expert_at<TPR, VEC>(i, t);
+        g[i] = e < a.experts ? bf * (float)a.counts[e] : 0.0f;
+    }
+    __syncwarp();
+    for (uint64_t base = (uint64_t)blockIdx.x * TEAMS; base < a.n; base += (uint64_t)gridDim.x * TEAMS) {
+        const uint64_t row = base + team;
+        const bool in = row < a.n;
+        const bool on = in && (!a.active || a.active[row]);
+        const X* logits = (const X*)a.logits + row * a.stride;
+        const float lse = on ? a.lse[row] : 0.0f;
+        float x[EPT];
+        load_logits<X, VEC, TPR, EPT>(logits, on, a.experts, t, -CUDART_INF_F, x);
+        int32_t c[SLOTS];
+        float p_c[SLOTS], dw[SLOTS], part = 0, kept = 0;
+        if (a.dweight) {
+#pragma unroll
+            for (int s = 0; s < SLOTS; ++s) {
+                const uint32_t j = s * TPR + t;
+                c[s] = on && j < a.top ? a.choice[row * a.top + j] : -1;
+                if ((uint32_t)c[s] >= a.experts) c[s] = -1;
+                dw[s] = c[s] >= 0 ? a.dweight[row * a.top + j] : 0.0f;
+                p_c[s] = c[s] >= 0 ? __expf(widen<float>(logits[c[s]]) - lse) : 0.0f;
+                part += dw[s] * p_c[s];
+                kept += p_c[s];
+            }
+            if (a.renormalize) {
+                kept = lanes_sum<TPR>(kept);
+                const float inv = kept != 0.0f ? 1.0f / kept : 0.0f;
+                const float mean = lanes_sum<TPR>(part) * inv;
+                part = 0.0f;
+#pragma unroll
+                for (int s = 0; s < SLOTS; ++s) p_c[s] *= inv * (dw[s] - mean);
+            } else {
+#pragma unroll
+                for (int s = 0; s < SLOTS; ++s) p_c[s] *= dw[s];
+            }
+#pragma unroll
+            for (int s = 0; s < SLOTS; ++s)
+                if (c[s] >= 0) atomicAdd(&extra[team][c[s]], p_c[s]);
+            __syncwarp();
+        }
+        float p[EPT];
+#pragma unroll
+        for (int i = 0; i < EPT; ++i) {
+            p[i] = __expf(x[i] - lse);
+            part += g[i] * p[i];
+        }
+        const float off = zf * lse - lanes_sum<TPR>(part);
+        if (in) {
+#pragma unroll
+            for (int k = 0; k < EPT / VEC; ++k) {
+                const uint32_t e = expert_at<TPR, VEC>(k * VEC, t);
+                if (e < a.experts) {
+                    float d[VEC];
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) {
+                        d[j] = on ? p[k * VEC + j] * (g[k * VEC + j] + off) : 0.0f;
+                        if (a.dweight) d[j] += extra[team][e + j];
+                    }
+                    store_values<X, VEC>((X*)a.dlogits + row * a.dstride + e, d);
+                }
+            }
+        }
+        if (a.dweight) {
+            __syncwarp();
+#pragma unroll
+            for (int s = 0; s < SLOTS; ++s)
+                if (c[s] >= 0) extra[team][c[s]] = 0.0f;
+            __syncwarp();
+        }
+    }
+}
+
+template <class... KArgs> unsigned resident_blocks(void (*kernel)(KArgs...))
+{
+    int n = 0;
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, ROUTE_BLOCK, 0) != cudaSuccess) cudaGetLastError();
+    return n > 0 ? (unsigned)n : 1u;
+}
+
+uint32_t route_teams(uint32_t experts) { return experts <= 16 ? 64 : experts <= 128 ? 32 : 8; }
+// Blocks that leave sums: a rule on the sizes alone, so that the order of the additions is theirs too.
+unsigned route_blocks(const nups_store* s, uint64_t n, uint32_t experts)
+{
+    return grid_for(n, route_teams(experts), (unsigned)s->sm_count * (experts <= 256 ? 4 : experts <= 512 ? 3 : 2));
+}
+
+// Do rows of logits allow runs of VEC?
+bool route_wide(const void* p, uint64_t stride, uint32_t experts, uint64_t n, int bytes, int vec)
+{
+    return experts % vec == 0 && ((uintptr_t)p & (bytes * vec - 1)) == 0 && (n <= 1 || stride % vec == 0);
+}
+
+template <class X>
+nups_status launch_route(nups_store* s, const RouteArgs& a, cudaStream_t st)
+{
+    const unsigned blocks = route_blocks(s, a.n, a.experts);
+    constexpr int V = 16 / sizeof(X);
+    const bool wide = route_wide(a.logits, a.stride, a.experts, a.n, sizeof(X), a.experts <= 16 ? 4 : V);
+#define NUPS_ROUTE(TPR_, EPT_, V_)                                                                                    \
+    {                                                                                                                 \
+        if (wide) nups_launch_dependent(route_kernel<X, V_, TPR_, EPT_>, blocks, ROUTE_BLOCK, 0, st, a);              \
+        else nups_launch_dependent(route_kernel<X, 1, TPR_, EPT_>, blocks, ROUTE_BLOCK, 0, st, a);                    \
+    }
+    if (a.experts <= 16) NUPS_ROUTE(4, 4, 4)
+    else if (a.experts <= 64) NUPS_ROUTE(8, 8, V)
+    else if (a.experts <= 128) NUPS_ROUTE(8, 16, V)
+    else if (a.experts <= 256) NUPS_ROUTE(32, 8, V)
+    else if (a.experts <= 512) NUPS_ROUTE(32, 16, V)
+    else NUPS_ROUTE(32, 32, V)
+#undef NUPS_ROUTE
+    LAUNCH_CHECK(s);
+    if (blocks == 1) return NUPS_OK;
+    uint32_t width = 32;
+    while (width * JOIN_CLUSTER < a.experts) width *= 2;
+    nups_launch_dependent(route_join_kernel, JOIN_CLUSTER, JOIN_BLOCK, 0, st, a, blocks, width);
+    LAUNCH_CHECK(s);
+    return NUPS_OK;
+}
+
+template <class X>
+nups_status launch_route_grad(nups_store* s, const RouteGradArgs& a, cudaStream_t st)
+{
+    constexpr int V = 16 / sizeof(X);
+    const int v = a.experts <= 16 ? 4 : V;
+    const bool wide = route_wide(a.logits, a.stride, a.experts, a.n, sizeof(X), v) && route_wide(a.dlogits, a.dstride, a.experts, a.n, sizeof(X), v);
+#define NUPS_ROUTE(TPR_, EPT_, V_)                                                                                                     \
+    {                                                                                                                                  \
+        static const unsigned resident = resident_blocks(route_grad_kernel<X, V_, TPR_, EPT_>);                                        \
+        const unsigned blocks = grid_for(a.n, ROUTE_BLOCK / TPR_, (unsigned)s->sm_count * resident);                                   \
+        if (wide) nups_launch_dependent(route_grad_kernel<X, V_, TPR_, EPT_>, blocks, ROUTE_BLOCK, 0, st, a);                          \
+        else nups_launch_dependent(route_grad_kernel<X, 1, TPR_, EPT_>, blocks, ROUTE_BLOCK, 0, st, a);                                \
+    }
+    if (a.experts <= 16) NUPS_ROUTE(4, 4, 4)
+    else if (a.experts <= 64) NUPS_ROUTE(8, 8, V)
+    else if (a.experts <= 128) NUPS_ROUTE(8, 16, V)
+    else if (a.experts <= 256) NUPS_ROUTE(32, 8, V)
+    else if (a.experts <= 512) NUPS_ROUTE(32, 16, V)
+    else NUPS_ROUTE(32, 32, V)
+#undef NUPS_ROUTE
+    LAUNCH_CHECK(s);
+    return NUPS_OK;
+}
+
+bool route_sizes(int type, uint64_t stride, uint64_t n, uint32_t experts, uint32_t top, float balance, float z)
+{
+    return (type == NUPS_F32 || type == NUPS_F16 || type == NUPS_BF16) && experts >= 1 && experts <= NUPS_ROUTE_MAX_EXPERTS && top >= 1 && top <= experts &&
+           top <= NUPS_ROUTE_MAX_TOP && n < (1ull << 32) && stride < (1ull << 32) && (n <= 1 || stride >= experts) && isfinite(balance) && isfinite(z);
+}
+
+}  // namespace
+
+extern "C" nups_status nups_route_scratch(nups_store* s, uint64_t n, uint32_t experts, uint64_t* h_bytes_out)
+{
+    if (!s || !h_bytes_out || experts < 1 || experts > NUPS_ROUTE_MAX_EXPERTS || n >= (1ull << 32)) return NUPS_EINVAL;
+    *h_bytes_out = (uint64_t)route_blocks(s, n, experts) * (experts + 1) * 8;
+    return NUPS_OK;
+}
+
+extern "C" nups_status nups_route(nups_store* s, const void* d_logits, int type, uint64_t stride, uint64_t n, uint32_t experts, uint32_t top,
+                                  const uint8_t* d_active, int renormalize, float balance, float z, int32_t* d_choice, float* d_weight,
+                                  float* d_lse, uint64_t* d_counts, uint64_t* d_tokens, float* d_prob, float* d_loss, void* d_scratch,
+                                  uint64_t scratch_bytes, void* stream)
+{
+    if (!s || !route_sizes(type, stride, n, experts, top, balance, z) || !d_counts || !d_tokens) return NUPS_EINVAL;
+    if (n && (!d_logits || !d_choice || !d_weight)) return NUPS_EINVAL;
+    uint64_t bytes = 0;
+    nups_route_scratch(s, n, experts, &bytes);
+    if (n && (!d_scratch || scratch_bytes < bytes || ((uintptr_t)d_scratch & 255))) return NUPS_EINVAL;
+    nups_status rc = on_own_device(s);
+    if (rc != NUPS_OK) return rc;
+    cudaStream_t st = (cudaStream_t)stream;
+    if (n == 0) {
+        CK(cudaMemsetAsync(d_counts, 0, experts * sizeof(uint64_t), st));
+        CK(cudaMemsetAsync(d_tokens, 0, sizeof(uint64_t), st));
+        if (d_prob) CK(cudaMemsetAsync(d_prob, 0, experts * sizeof(float), st));
+        if (d_loss) CK(cudaMemsetAsync(d_loss, 0, 3 * sizeof(float), st));
+        return NUPS_OK;
+    }
+    const uint64_t cells = (uint64_t)route_blocks(s, n, experts) * (experts + 1);
+    RouteArgs a = {d_logits, stride, n, experts, top, d_active, renormalize != 0, d_prob || d_loss, balance, z, d_choice, d_weight, d_lse, d_counts, d_tokens,
+                   d_prob, d_loss, (float*)d_scratch, (uint32_t*)d_scratch + cells};
+    return type == NUPS_F32 ? launch_route<float>(s, a, st) : type == NUPS_F16 ? launch_route<__half>(s, a, st) : launch_route<__nv_bfloat16>(s, a, st);
+}
+
+extern "C" nups_status nups_route_grad(nups_store* s, const void* d_logits, int type, uint64_t stride, uint64_t n, uint32_t experts, uint32_t top,
+                                       const uint8_t* d_active, int renormalize, float balance, float z, const int32_t* d_choice,
+                                       const float* d_lse, const uint64_t* d_counts, const uint64_t* d_tokens, const float* d_dloss,
+                                       const float* d_dweight, void* d_dlogits, uint64_t dlogits_stride, void* stream)
+{
+    if (!s || !route_sizes(type, stride, n, experts, top, balance, z) || !route_sizes(type, dlogits_stride, n, experts, top, 0, 0)) return NUPS_EINVAL;
+    if (n && (!d_logits || !d_lse || !d_counts || !d_tokens || !d_dlogits || (d_dweight && !d_choice))) return NUPS_EINVAL;
+    nups_status rc = on_own_device(s);
+    if (rc != NUPS_OK || n == 0) return rc;
+    RouteGradArgs a = {d_logits, stride, n, experts, top, d_active, renormalize != 0, balance, z, d_choice, d_lse, d_counts, d_tokens, d_dloss, d_dweight,
+                       d_dlogits, dlogits_stride};
+    cudaStream_t st = (cudaStream_t)stream;
+    return type == NUPS_F32 ? launch_route_grad<float>(s, a, st)
+                            : type == NUPS_F16 ? launch_route_grad<__half>(s, a, st) : launch_route_grad<__nv_bfloat16>(s, a, st);
+}
