@@ -444,6 +444,35 @@ nups_status nups_route_grad(nups_store* store, const void* d_logits, int type, u
                             const float* d_lse, const uint64_t* d_counts, const uint64_t* d_tokens, const float* d_dloss,
                             const float* d_dweight, void* d_dlogits, uint64_t dlogits_stride, void* stream);
 
+/* Orthogonalized update (Newton-Schulz products): for each of `batch` matrices G of
+ * rows x cols values
+ *   X = G / (|G| + eps)                       |G|: root of the sum of squares
+ *   X = a X + (b X X^T + c (X X^T)^2) X       `steps` times
+ *   out = scale X
+ * (for rows > cols the transposed matrix is iterated, which is the same with
+ * smaller products).  Each singular value s of G / |G| becomes the polynomial's
+ * iterate, its singular vectors stay; with coefficients such as (3.4445, -4.7750,
+ * 2.0315) and 5 steps all but the smallest come close to 1.  Meant for a row of a
+ * store that holds a matrix: scale = -rate makes out the delta that nups_push adds
+ * (fp32 out, row-major, as the store's rows are).
+ * type (NUPS_F32, NUPS_F16, NUPS_BF16) is that of G and out.  Row i of matrix k
+ * starts at k * batch_stride + i * stride VALUES; the values of a row are
+ * contiguous.  out may be G (same strides).  Products are formed from pairs of
+ * fp16 values that hold 22 bits of each number, with fp32 sums.  A matrix of
+ * zeros gives zeros; NaN or infinity in a matrix makes that matrix NaN.
+ * h_coefficients = {a, b, c}.  1 <= steps <= NUPS_ORTHOGONALIZE_MAX_STEPS, eps > 0,
+ * 1 <= rows, cols <= NUPS_ORTHOGONALIZE_MAX_SIZE, batch <= 65535.  NUPS_EINVAL also when
+ * the iteration with these coefficients carries a singular value from [0, 1]
+ * above 2.5, or a factor a + b s^2 + c s^4 above 7.5: its products would leave the
+ * range of the fp16 pairs.                                                      */
+#define NUPS_ORTHOGONALIZE_MAX_STEPS 64
+#define NUPS_ORTHOGONALIZE_MAX_SIZE 65536
+nups_status nups_orthogonalize(nups_store* store, const void* d_update, int type, uint64_t stride, uint64_t batch_stride, uint32_t batch,
+                               uint32_t rows, uint32_t cols, uint32_t steps, const float* h_coefficients, float eps, float scale,
+                               void* d_out, uint64_t out_stride, uint64_t out_batch_stride, void* d_scratch, uint64_t scratch_bytes,
+                               void* stream);
+nups_status nups_orthogonalize_scratch(nups_store* store, uint32_t batch, uint32_t rows, uint32_t cols, uint64_t* h_bytes_out);
+
 /* ---- status and statistics ------------------------------------------------ */
 
 /* Read and clear the device status word (synchronises the stream): NUPS_OK,

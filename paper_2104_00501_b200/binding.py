@@ -33,6 +33,7 @@ EXPORTS = [
     "nups_shard_last_error", "nups_merge_mark", "nups_merge_export", "nups_merge_apply",
     "nups_layer_norm", "nups_pull_norm", "nups_layer_norm_grad", "nups_layer_norm_grad_scratch",
     "nups_route", "nups_route_scratch", "nups_route_grad",
+    "nups_orthogonalize", "nups_orthogonalize_scratch",
 ]
 
 
@@ -122,6 +123,8 @@ def load(build_if_missing: bool = True):
         "nups_pull_norm": [vp, vp, u64, vp, vp, C.c_double, vp, C.c_int, vp, vp, vp, vp],
         "nups_layer_norm_grad": [vp, vp, C.c_int, u64, vp, C.c_int, u64, u64, u32, vp, vp, vp, C.c_int, vp, u64, vp, vp, vp, u64, vp],
         "nups_layer_norm_grad_scratch": [vp, u64, u32, C.c_int, C.POINTER(u64)],
+        "nups_orthogonalize": [vp, vp, C.c_int, u64, u64, u32, u32, u32, u32, C.POINTER(f32), f32, f32, vp, u64, u64, vp, u64, vp],
+        "nups_orthogonalize_scratch": [vp, u32, u32, u32, C.POINTER(u64)],
         "nups_route": [vp, vp, C.c_int, u64, u64, u32, u32, vp, C.c_int, f32, f32, vp, vp, vp, vp, vp, vp, vp, vp, u64, vp],
         "nups_route_scratch": [vp, u64, u32, C.POINTER(u64)],
         "nups_route_grad": [vp, vp, C.c_int, u64, u64, u32, u32, vp, C.c_int, f32, f32, vp, vp, vp, vp, vp, vp, vp, u64, vp],
@@ -523,6 +526,30 @@ class Store:
         self._chk(self._l.nups_route_grad(self._s, p, _type(logits), stride, n, experts, top, self._active(w, r.active, n), int(r.renormalize), r.balance,
                                           r.z, _ptr(r.choice), self._vector(w, r.lse, n), _ptr(r.counts, torch.int64), _ptr(r.tokens, torch.int64),
                                           _ptr(dloss), _ptr(dweight), po, os_, _stream()), w)
+        return out
+
+    def orthogonalize(self, update, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7, scale=1.0, out=None):
+        """`scale` times the Newton-Schulz iterate of a matrix [rows, cols] or of a batch of them [batch, rows, cols]; out may be
+        the update itself.  What push adds to rows that hold matrices: scale = -rate, out as [batch, rows * cols]."""
+        w = "nups_orthogonalize"
+        if out is None:
+            out = torch.empty(update.shape, dtype=update.dtype, device=update.device)
+        self._on_device(w, update, out)
+        if update.dim() not in (2, 3) or out.shape != update.shape or out.dtype != update.dtype or len(coefficients) != 3:
+            raise NupsError(EINVAL, w, "expected a matrix or a batch of them, out of the same shape and type, three coefficients")
+        (batch, rows, cols), places = (1,) * (3 - update.dim()) + tuple(update.shape), []
+        for t in (update, out):
+            if cols > 1 and t.stride(-1) != 1:
+                raise NupsError(EINVAL, w, "the values of a row must be contiguous")
+            places.append((t.data_ptr(), t.stride(-2) if rows > 1 else cols, t.stride(0) if batch > 1 and t.dim() == 3 else 0))
+            if places[-1][1] < 0 or places[-1][2] < 0:
+                raise NupsError(EINVAL, w, "strides must not be negative")
+        size = C.c_uint64()
+        self._chk(self._l.nups_orthogonalize_scratch(self._s, batch, rows, cols, C.byref(size)), w)
+        scratch = torch.empty(size.value, dtype=torch.uint8, device=update.device)
+        (pg, gs, gb), (po, os_, ob) = places
+        self._chk(self._l.nups_orthogonalize(self._s, pg, _type(update), gs, gb, batch, rows, cols, steps, (C.c_float * 3)(*coefficients), eps, scale,
+                                             po, os_, ob, _ptr(scratch), size.value, _stream()), w)
         return out
 
     # -- status -------------------------------------------------------------------------
