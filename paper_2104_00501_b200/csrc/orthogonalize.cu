@@ -47,6 +47,25 @@ __device__ __forceinline__ void split(float x, __half& hi, __half& lo)
     hi = __float2half_rn(x);
     lo = __float2half_rn(x - __half2float(hi));
 }
+// Eight values into eight pairs, and back.
+__device__ __forceinline__ void split8(const float* v, uint4& hi, uint4& lo)
+{
+    uint32_t* h = (uint32_t*)&hi;
+    uint32_t* l = (uint32_t*)&lo;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const __half2 a = __floats2half2_rn(v[2 * k], v[2 * k + 1]);
+        const float2 f = __half22float2(a);
+        const __half2 b = __floats2half2_rn(v[2 * k] - f.x, v[2 * k + 1] - f.y);
+        h[k] = *(const uint32_t*)&a;
+        l[k] = *(const uint32_t*)&b;
+    }
+}
+__device__ __forceinline__ float2 join2(uint32_t hi, uint32_t lo)
+{
+    const float2 a = __half22float2(*(const __half2*)&hi), b = __half22float2(*(const __half2*)&lo);
+    return make_float2(a.x + b.x, a.y + b.y);
+}
 __device__ __forceinline__ double warp_sum_f64(double x)
 {
 #pragma unroll
@@ -166,12 +185,11 @@ __global__ void __launch_bounds__(SMALL_BLOCK) orthogonalize_small_kernel(OrthAr
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             if (c0 + 8 * k < width) {
-                __align__(16) __half hi[8], lo[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) split(v[8 * k + j], hi[j], lo[j]);
+                uint4 hi, lo;
+                split8(v + 8 * k, hi, lo);
                 const uint32_t at = panel_at(row, c0 + 8 * k);
-                *(uint4*)(hi_base + at) = *(const uint4*)hi;
-                *(uint4*)(lo_base + at) = *(const uint4*)lo;
+                *(uint4*)(hi_base + at) = hi;
+                *(uint4*)(lo_base + at) = lo;
             }
         }
     };
@@ -199,14 +217,14 @@ __global__ void __launch_bounds__(SMALL_BLOCK) orthogonalize_small_kernel(OrthAr
             for (int k = 0; k < 4; ++k) {
                 if (c0 + 8 * k < m16) {
                     const uint32_t at = panel_at(row, c0 + 8 * k);
-                    __align__(16) __half hi[8], lo[8];
-                    *(uint4*)hi = *(const uint4*)(a_hi + at);
-                    *(uint4*)lo = *(const uint4*)(a_lo + at);
+                    const uint4 hi = *(const uint4*)(a_hi + at), lo = *(const uint4*)(a_lo + at);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float old = __half2float(hi[j]) + __half2float(lo[j]);
-                        const uint32_t c = c0 + 8 * k + j;
-                        v[8 * k + j] = a.b * old + a.c * (v[8 * k + j] * (FROM_AA * A_SCALE)) + (c == row && row < a.m ? a.a * A_SCALE : 0.0f);
+                    for (int j = 0; j < 4; ++j) {
+                        const float2 old = join2(((const uint32_t*)&hi)[j], ((const uint32_t*)&lo)[j]);
+                        const uint32_t c = c0 + 8 * k + 2 * j;
+                        float *x = v + 8 * k + 2 * j, diagonal = row < a.m ? a.a * A_SCALE : 0.0f;
+                        x[0] = a.b * old.x + a.c * (x[0] * (FROM_AA * A_SCALE)) + (c == row ? diagonal : 0.0f);
+                        x[1] = a.b * old.y + a.c * (x[1] * (FROM_AA * A_SCALE)) + (c + 1 == row ? diagonal : 0.0f);
                     }
                 }
             }
@@ -270,9 +288,12 @@ __global__ void __launch_bounds__(256) orth_squares_kernel(OrthArgs a, double* s
     const char* g = (const char*)a.g + (uint64_t)blockIdx.y * a.gb * (a.type == NUPS_F32 ? 4 : 2);
     double sum = 0;
     for (uint32_t r = blockIdx.x; r < a.rows; r += NORM_PARTS)
-        for (uint32_t c = threadIdx.x; c < a.cols; c += 256) {
-            const float x = read_value(g, a.type, (uint64_t)r * a.gs + c);
-            sum += (double)x * x;
+        for (uint32_t c = threadIdx.x; c < a.cols; c += 256 * 8) {
+            float x[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = c + 256 * k < a.cols ? read_value(g, a.type, (uint64_t)r * a.gs + c + 256 * k) : 0.0f;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum += (double)x[k] * x[k];
         }
     sum = warp_sum_f64(sum);
     if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = sum;
@@ -434,10 +455,13 @@ orth_tiled_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                     tma_load(to + 2 * A_BYTES + p * B_BYTES, &map_b, MN_MAJOR ? n0 : k0, MN_MAJOR ? k0 : n0, z + p, full(s));
                 }
             }
-            // copies in flight must land before the block ends; usually all have
-            for (uint32_t k = kb > STAGES ? kb - STAGES : 0; k < kb; ++k) ok &= mbar_wait(full(k % STAGES), (k / STAGES) & 1);
-            if (MODE == POLYNOMIAL && ok) {                 // A's tile, where the result is going to be put together
-                for (uint32_t k = kb > STAGES ? kb - STAGES : 0; k < kb; ++k) ok &= mbar_wait(empty(k % STAGES), (k / STAGES) & 1);
+            // Whatever still comes to this block's shared memory must come before it ends: the copies in flight, and the products'
+            // signals that a stage is free, which nobody else waits for at the end (a later block's barriers may lie at that place).
+            for (uint32_t k = kb > STAGES ? kb - STAGES : 0; k < kb; ++k) {
+                ok &= mbar_wait(full(k % STAGES), (k / STAGES) & 1);
+                ok &= mbar_wait(empty(k % STAGES), (k / STAGES) & 1);
+            }
+            if (MODE == POLYNOMIAL) {                       // A's tile, where the result is going to be put together
                 if (ok) {
                     mbar_expect(old_here, 4 * PANEL);
                     for (int p = 0; p < 2; ++p)
@@ -532,21 +556,25 @@ orth_tiled_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
 #pragma unroll
             for (int c = 0; c < OWN; c += 8) {
                 const uint32_t at = panel_at(own_row, c);
-                __align__(16) __half hi[8], lo[8];
+                uint4 hi, lo;
+                float* v = acc + c;
                 if (MODE == POLYNOMIAL) {
-                    *(uint4*)hi = *(const uint4*)(hi_panel + at);
-                    *(uint4*)lo = *(const uint4*)(lo_panel + at);
-                }
+                    hi = *(const uint4*)(hi_panel + at);
+                    lo = *(const uint4*)(lo_panel + at);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    float& v = acc[c + j];
-                    if (MODE == GRAM) v *= FROM_XX * A_SCALE;
-                    else if (MODE == PRODUCT) v *= FROM_BX * X_SCALE;
-                    else v = o.b * (__half2float(hi[j]) + __half2float(lo[j])) + o.c * (v * (FROM_AA * A_SCALE)) + (col + c + j == row0 + own_row ? o.a * A_SCALE : 0.0f);
-                    split(v, hi[j], lo[j]);
+                    for (int j = 0; j < 4; ++j) {
+                        const float2 old = join2(((const uint32_t*)&hi)[j], ((const uint32_t*)&lo)[j]);
+                        const uint32_t k = col + c + 2 * j, r = row0 + own_row;
+                        v[2 * j] = o.b * old.x + o.c * (v[2 * j] * (FROM_AA * A_SCALE)) + (k == r ? o.a * A_SCALE : 0.0f);
+                        v[2 * j + 1] = o.b * old.y + o.c * (v[2 * j + 1] * (FROM_AA * A_SCALE)) + (k + 1 == r ? o.a * A_SCALE : 0.0f);
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] *= MODE == GRAM ? FROM_XX * A_SCALE : FROM_BX * X_SCALE;
                 }
-                *(uint4*)(hi_panel + at) = *(const uint4*)hi;
-                *(uint4*)(lo_panel + at) = *(const uint4*)lo;
+                split8(v, hi, lo);
+                *(uint4*)(hi_panel + at) = hi;
+                *(uint4*)(lo_panel + at) = lo;
             }
             const bool first = (threadIdx.x & 127) == 64;   // warps 2 to 5 and 6 to 9: one thread of each group
             const int z = 2 * (int)blockIdx.y;
@@ -601,14 +629,24 @@ __global__ void __launch_bounds__(256) orth_join_kernel(const float* part, uint3
     const uint32_t tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
     __half* hi = a + (uint64_t)blockIdx.z * 2 * m * ld;
     __half* lo = hi + (uint64_t)m * ld;
-    for (uint32_t k = ty; k < 64; k += 4) {
-        const uint32_t r = r0 + k, c = c0 + tx;
+    float v[16];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) v[k] = 0.0f;
+    for (uint32_t s = 0; s < slices; ++s) {
+        const float* from = part + ((uint64_t)s * batch + blockIdx.z) * m * ld + c0 + tx;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            const uint32_t r = r0 + ty + 4 * k;
+            if (r < m && c0 + tx < m) v[k] += __ldcg(from + (uint64_t)r * ld);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+        const uint32_t r = r0 + ty + 4 * k, c = c0 + tx;
+        tile[ty + 4 * k][tx] = v[k];
         if (r < m && c < m) {
-            float v = 0.0f;
-            for (uint32_t s = 0; s < slices; ++s) v += __ldcg(part + (((uint64_t)s * batch + blockIdx.z) * m + r) * ld + c);
-            tile[k][tx] = v;
             __half h, l;
-            split(v, h, l);
+            split(v[k], h, l);
             hi[(uint64_t)r * ld + c] = h;
             lo[(uint64_t)r * ld + c] = l;
         }
