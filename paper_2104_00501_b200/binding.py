@@ -167,9 +167,15 @@ def as_keys(t) -> torch.Tensor:
 
 
 def _type(t) -> int:
-    if t.dtype not in TYPES:
+    v = TYPES.get(t.dtype)
+    if v is None:
         raise NupsError(EINVAL, "value type", f"{t.dtype} is none of {', '.join(map(str, TYPES))}")
-    return TYPES[t.dtype]
+    return v
+
+
+# Scratch of one call from torch's allocator, on the call's stream and (while one is captured) in its graph's pool: given back as
+# soon as the call's work is enqueued, later work of the stream may have it.  A fourth of the host time of a tensor.
+_scratch_alloc, _scratch_free = torch._C._cuda_cudaCachingAllocator_raw_alloc, torch._C._cuda_cudaCachingAllocator_raw_delete
 
 
 class Routing(NamedTuple):
@@ -207,6 +213,7 @@ class Store:
         self.with_adagrad = bool(with_adagrad)
         self.dtype = torch.float64 if value_bytes == 8 else torch.float32       # what every value buffer holds
         self.device = torch.device("cuda", torch.cuda.current_device())
+        self._index, self._scratch_sizes = self.device.index, {}
 
     def _chk(self, code, what):
         if code != OK:
@@ -391,91 +398,139 @@ class Store:
         return torch.as_tensor(_Raw(), device=self.device).clone()
 
     # -- operators on model tensors -----------------------------------------------------
-    # All tensors are on the store's device, which is the current one; the calls run on its current stream.
+    # All tensors are on the store's device, which is the current one; the calls run on its current stream.  Small calls are
+    # bound by the host, so the checks are written for the case that passes.
     def _on_device(self, what, *tensors):
-        if torch._C._cuda_getDevice() != self.device.index:
+        here = self._index
+        if torch._C._cuda_getDevice() != here:
             raise NupsError(ESTATE, what, f"the store is on {self.device}, which is not the current device")
         for t in tensors:
-            if t is not None and t.device != self.device:
+            if t is not None and (not t.is_cuda or t.get_device() != here):
                 raise NupsError(EINVAL, what, f"a tensor is on {t.device}, the store on {self.device}")
+
+    def _scratch_bytes(self, fn, *sizes):
+        """What a *_scratch call names for these sizes; asked for once per store."""
+        key = (fn, *sizes)
+        n = self._scratch_sizes.get(key)
+        if n is None:
+            size = C.c_uint64()
+            self._chk(getattr(self._l, fn)(self._s, *sizes, C.byref(size)), fn)
+            if len(self._scratch_sizes) >= 4096:
+                self._scratch_sizes.clear()
+            n = self._scratch_sizes[key] = size.value
+        return n
 
     def _rows(self, what, t, n=None, length=None):
         """(address, stride) of a matrix whose rows are contiguous; rows may lie apart from one another."""
-        if t.dim() != 2 or (n is not None and tuple(t.shape) != (n, length)):
-            raise NupsError(EINVAL, what, f"expected a matrix{'' if n is None else f' of {n} x {length}'}, got {tuple(t.shape)}")
-        if t.shape[1] > 1 and t.stride(1) != 1:
+        shape = t.shape
+        if len(shape) != 2 or (n is not None and (shape[0] != n or shape[1] != length)):
+            raise NupsError(EINVAL, what, f"expected a matrix{'' if n is None else f' of {n} x {length}'}, got {tuple(shape)}")
+        stride, step = t.stride()
+        if step != 1 and shape[1] > 1:
             raise NupsError(EINVAL, what, "the values of a row must be contiguous")
-        stride = t.stride(0) if t.shape[0] > 1 else t.shape[1]
-        if stride < t.shape[1]:
+        if shape[0] <= 1:
+            stride = shape[1]
+        elif stride < shape[1]:
             raise NupsError(EINVAL, what, "rows must not overlap")
         return t.data_ptr(), stride
 
     def _vector(self, what, t, length, dtype=None):
         if t is None:
             return None
-        if tuple(t.shape) != (length,) or (length > 1 and t.stride(0) != 1) or (dtype is not None and t.dtype != dtype):
+        if t.dim() != 1 or t.shape[0] != length or (length > 1 and t.stride(0) != 1) or (dtype is not None and t.dtype != dtype):
             raise NupsError(EINVAL, what, f"expected {length} contiguous values{'' if dtype is None else f' of {dtype}'}, got {tuple(t.shape)} of {t.dtype}")
         return t.data_ptr()
 
     def _params(self, what, x_dtype, length, *vectors):
         """Type of the parameters given (x's type, or float32), and their addresses."""
-        given = [v for v in vectors if v is not None]
-        dtype = given[0].dtype if given else x_dtype
-        if any(v.dtype != dtype for v in given):
-            raise NupsError(EINVAL, what, "weight and bias must be of one type")
-        return dtype, [self._vector(what, v, length) for v in vectors]
+        dtype, at = None, []
+        for v in vectors:
+            if v is not None:
+                if dtype is None:
+                    dtype = v.dtype
+                elif v.dtype != dtype:
+                    raise NupsError(EINVAL, what, "weight and bias must be of one type")
+            at.append(self._vector(what, v, length))
+        return x_dtype if dtype is None else dtype, at
 
     def layer_norm(self, x, weight=None, bias=None, eps=1e-5, out_dtype=None, stats=True, out=None):
         """(y, mean, rstd) of the rows of x [n, len]; stats=False: y alone.  out may be x itself."""
         w = "nups_layer_norm"
         if out is None:
-            out = torch.empty(x.shape, dtype=out_dtype or x.dtype, device=x.device)
+            out = torch.empty_like(x) if out_dtype is None else torch.empty_like(x, dtype=out_dtype)
         self._on_device(w, x, weight, bias, out)
-        (px, xs), (py, ys) = self._rows(w, x), self._rows(w, out, *x.shape)
+        px, xs = self._rows(w, x)
         n, length = x.shape
+        py, ys = self._rows(w, out, n, length)
         dtype, (pw, pb) = self._params(w, x.dtype, length, weight, bias)
-        keep = torch.float64 if x.dtype == torch.float64 else torch.float32
-        mean, rstd = (torch.empty(n, dtype=keep, device=x.device) for _ in range(2)) if stats else (None, None)
-        self._chk(self._l.nups_layer_norm(self._s, px, _type(x), xs, n, length, pw, pb, TYPES.get(dtype, -1), eps, py, _type(out), ys,
-                                          _ptr(mean), _ptr(rstd), _stream()), w)
+        if stats:
+            keep = torch.float64 if x.dtype == torch.float64 else torch.float32
+            mean = torch.empty(n, dtype=keep, device=self.device)
+            rstd = torch.empty(n, dtype=keep, device=self.device)
+            pm, pr = mean.data_ptr(), rstd.data_ptr()
+        else:
+            pm = pr = None
+        rc = self._l.nups_layer_norm(self._s, px, _type(x), xs, n, length, pw, pb, TYPES.get(dtype, -1), eps, py, _type(out), ys, pm, pr, _stream())
+        if rc:
+            self._chk(rc, w)
         return (out, mean, rstd) if stats else out
 
     def pull_norm(self, keys, weight=None, bias=None, eps=1e-5, out_dtype=None, stats=True, rows=False):
         """Layer norm of the pulled rows: (y, mean, rstd), and with rows=True also the rows; stats=False: without mean and rstd."""
-        w, n = "nups_pull_norm", keys.numel()
+        w, n, mine = "nups_pull_norm", keys.numel(), self.dtype
         self._on_device(w, keys, weight, bias)
-        dtype, (pw, pb) = self._params(w, self.dtype, self.L, weight, bias)
-        if dtype != self.dtype:
-            raise NupsError(EINVAL, w, f"weight and bias must be of the store's type, {self.dtype}")
-        y = torch.empty((n, self.L), dtype=out_dtype or self.dtype, device=self.device)
-        pulled = torch.empty((n, self.L), dtype=self.dtype, device=self.device) if rows else None
-        mean, rstd = (torch.empty(n, dtype=self.dtype, device=self.device) for _ in range(2)) if stats else (None, None)
-        self._chk(self._l.nups_pull_norm(self._s, _ptr(keys, torch.int32), n, pw, pb, eps, _ptr(y), _type(y), _ptr(pulled), _ptr(mean),
-                                         _ptr(rstd), _stream()), w)
-        res = (y, mean, rstd) if stats else (y,)
-        res = res + (pulled,) if rows else res
-        return res if len(res) > 1 else y
+        dtype, (pw, pb) = self._params(w, mine, self.L, weight, bias)
+        if dtype != mine:
+            raise NupsError(EINVAL, w, f"weight and bias must be of the store's type, {mine}")
+        pk = _ptr(keys, torch.int32)
+        shape, strides = (n, self.L), (self.L, 1)
+        y = torch.empty_strided(shape, strides, dtype=out_dtype or mine, device=self.device)
+        pulled = mean = rstd = pp = pm = pr = None
+        if rows:
+            pulled = torch.empty_strided(shape, strides, dtype=mine, device=self.device)
+            pp = pulled.data_ptr()
+        if stats:
+            mean = torch.empty(n, dtype=mine, device=self.device)
+            rstd = torch.empty(n, dtype=mine, device=self.device)
+            pm, pr = mean.data_ptr(), rstd.data_ptr()
+        rc = self._l.nups_pull_norm(self._s, pk, n, pw, pb, eps, y.data_ptr(), _type(y), pp, pm, pr, _stream())
+        if rc:
+            self._chk(rc, w)
+        if stats:
+            return (y, mean, rstd, pulled) if rows else (y, mean, rstd)
+        return (y, pulled) if rows else y
 
     def layer_norm_grad(self, x, dy, mean, rstd, weight=None, need_dx=True, need_params=True, dx=None):
         """(dx, dweight, dbias) of layer_norm; what is not needed is None.  dweight and dbias have weight's type (x's without one)."""
         w = "nups_layer_norm_grad"
-        n, length = x.shape if x.dim() == 2 else (0, 0)
         if need_dx and dx is None:
-            dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+            dx = torch.empty_like(x)
         self._on_device(w, x, dy, mean, rstd, weight, dx)
-        (px, xs), (pdy, dys) = self._rows(w, x), self._rows(w, dy, n, length)
-        pdx, dxs = self._rows(w, dx, n, length) if dx is not None else (None, length)
-        if dx is not None and dx.dtype != x.dtype:
-            raise NupsError(EINVAL, w, "dx must have x's type")
+        px, xs = self._rows(w, x)
+        n, length = x.shape
+        pdy, dys = self._rows(w, dy, n, length)
+        pdx, dxs = None, length
+        if dx is not None:
+            pdx, dxs = self._rows(w, dx, n, length)
+            if dx.dtype != x.dtype:
+                raise NupsError(EINVAL, w, "dx must have x's type")
         keep = torch.float64 if x.dtype == torch.float64 else torch.float32
         pm, pr = self._vector(w, mean, n, keep), self._vector(w, rstd, n, keep)
         dtype, (pw,) = self._params(w, x.dtype, length, weight)
-        dweight, dbias = (torch.empty(length, dtype=dtype, device=x.device) for _ in range(2)) if need_params else (None, None)
-        size = C.c_uint64()
-        self._chk(self._l.nups_layer_norm_grad_scratch(self._s, n, length, _type(x), C.byref(size)), w)
-        scratch = torch.empty(size.value, dtype=torch.uint8, device=x.device)
-        self._chk(self._l.nups_layer_norm_grad(self._s, px, _type(x), xs, pdy, _type(dy), dys, n, length, pm, pr, pw, TYPES.get(dtype, -1), pdx, dxs,
-                                               _ptr(dweight), _ptr(dbias), _ptr(scratch), size.value, _stream()), w)
+        x_type, stream = _type(x), _stream()
+        dweight = dbias = pdw = pdb = None
+        if need_params:
+            dweight = torch.empty(length, dtype=dtype, device=self.device)
+            dbias = torch.empty(length, dtype=dtype, device=self.device)
+            pdw, pdb = dweight.data_ptr(), dbias.data_ptr()
+        size = self._scratch_bytes("nups_layer_norm_grad_scratch", n, length, x_type)
+        scratch = _scratch_alloc(size, stream) if size else None
+        rc = self._l.nups_layer_norm_grad(self._s, px, x_type, xs, pdy, _type(dy), dys, n, length, pm, pr, pw, TYPES.get(dtype, -1), pdx, dxs, pdw, pdb,
+                                          scratch, size, stream)
+        if scratch:
+            _scratch_free(scratch)
+        if rc:
+            self._chk(rc, w)
         return dx, dweight, dbias
 
     def _active(self, what, active, n):
@@ -485,24 +540,32 @@ class Store:
             raise NupsError(EINVAL, what, f"active must be bool or uint8, got {active.dtype}")
         return self._vector(what, active, n)
 
-    def route(self, logits, top, active=None, renormalize=False, balance=0.0, z=0.0, losses=True):
-        """Softmax over experts and choice of the `top` largest of every item; see Routing.  losses=False (a program that only
-        answers): without prob, loss and lse."""
+    def route(self, logits, top, active=None, renormalize=False, balance=0.0, z=0.0, losses=None):
+        """Softmax over experts and choice of the `top` largest of every item; see Routing.  losses: with prob, loss and lse, which
+        route_grad needs; by default where balance or z is not 0 (a program that only answers does without)."""
         w = "nups_route"
         self._on_device(w, logits, active)
         p, stride = self._rows(w, logits)
         n, experts = logits.shape
         pa = self._active(w, active, n)
-        dev = logits.device
-        choice = torch.empty((n, top), dtype=torch.int32, device=dev)
-        weight = torch.empty((n, top), dtype=torch.float32, device=dev)
+        kind, dev = _type(logits), self.device
+        if not 0 < top <= experts:
+            raise NupsError(EINVAL, w, f"{top} of {experts} experts")
+        choice = torch.empty_strided((n, top), (top, 1), dtype=torch.int32, device=dev)
+        weight = torch.empty_like(choice, dtype=torch.float32)
         counts, tokens = torch.empty(experts, dtype=torch.int64, device=dev), torch.empty((), dtype=torch.int64, device=dev)
-        prob, loss, lse = (torch.empty(k, dtype=torch.float32, device=dev) for k in (experts, 3, n)) if losses else (None, None, None)
-        size = C.c_uint64()
-        self._chk(self._l.nups_route_scratch(self._s, n, experts, C.byref(size)), w)
-        scratch = torch.empty(size.value, dtype=torch.uint8, device=dev)
-        self._chk(self._l.nups_route(self._s, p, _type(logits), stride, n, experts, top, pa, int(renormalize), balance, z, _ptr(choice), _ptr(weight),
-                                     _ptr(lse), _ptr(counts), _ptr(tokens), _ptr(prob), _ptr(loss), _ptr(scratch), size.value, _stream()), w)
+        prob = loss = lse = pp = pl = pe = None
+        if losses or (losses is None and (balance != 0.0 or z != 0.0)):
+            prob, loss, lse = (torch.empty(k, dtype=torch.float32, device=dev) for k in (experts, 3, n))
+            pp, pl, pe = prob.data_ptr(), loss.data_ptr(), lse.data_ptr()
+        size, stream = self._scratch_bytes("nups_route_scratch", n, experts), _stream()
+        scratch = _scratch_alloc(size, stream) if size else None
+        rc = self._l.nups_route(self._s, p, kind, stride, n, experts, top, pa, renormalize, balance, z, choice.data_ptr(), weight.data_ptr(), pe,
+                                counts.data_ptr(), tokens.data_ptr(), pp, pl, scratch, size, stream)
+        if scratch:
+            _scratch_free(scratch)
+        if rc:
+            self._chk(rc, w)
         return Routing(choice, weight, counts, tokens, prob, loss, lse, active, renormalize, balance, z)
 
     def route_grad(self, logits, routing, dweight=None, dloss=None, out=None):
@@ -510,8 +573,9 @@ class Store:
         route gave for these logits; its counts and tokens may have been added up over several processes."""
         w, r = "nups_route_grad", routing
         if r.lse is None:
-            raise NupsError(EINVAL, w, "the forward call was made with losses=False")
-        out = torch.empty_like(logits, memory_format=torch.contiguous_format) if out is None else out
+            raise NupsError(EINVAL, w, "the forward call left out the losses")
+        if out is None:
+            out = torch.empty_like(logits)
         self._on_device(w, logits, r.choice, r.active, dweight, dloss, out)
         p, stride = self._rows(w, logits)
         n, experts = logits.shape
@@ -533,7 +597,7 @@ class Store:
         the update itself.  What push adds to rows that hold matrices: scale = -rate, out as [batch, rows * cols]."""
         w = "nups_orthogonalize"
         if out is None:
-            out = torch.empty(update.shape, dtype=update.dtype, device=update.device)
+            out = torch.empty_like(update, memory_format=torch.contiguous_format)
         self._on_device(w, update, out)
         if update.dim() not in (2, 3) or out.shape != update.shape or out.dtype != update.dtype or len(coefficients) != 3:
             raise NupsError(EINVAL, w, "expected a matrix or a batch of them, out of the same shape and type, three coefficients")
@@ -544,12 +608,16 @@ class Store:
             places.append((t.data_ptr(), t.stride(-2) if rows > 1 else cols, t.stride(0) if batch > 1 and t.dim() == 3 else 0))
             if places[-1][1] < 0 or places[-1][2] < 0:
                 raise NupsError(EINVAL, w, "strides must not be negative")
-        size = C.c_uint64()
-        self._chk(self._l.nups_orthogonalize_scratch(self._s, batch, rows, cols, C.byref(size)), w)
-        scratch = torch.empty(size.value, dtype=torch.uint8, device=update.device)
+        size = self._scratch_bytes("nups_orthogonalize_scratch", batch, rows, cols)
         (pg, gs, gb), (po, os_, ob) = places
-        self._chk(self._l.nups_orthogonalize(self._s, pg, _type(update), gs, gb, batch, rows, cols, steps, (C.c_float * 3)(*coefficients), eps, scale,
-                                             po, os_, ob, _ptr(scratch), size.value, _stream()), w)
+        stream, kind = _stream(), _type(update)
+        scratch = _scratch_alloc(size, stream) if size else None
+        rc = self._l.nups_orthogonalize(self._s, pg, kind, gs, gb, batch, rows, cols, steps, (C.c_float * 3)(*coefficients), eps, scale, po, os_, ob,
+                                        scratch, size, stream)
+        if scratch:
+            _scratch_free(scratch)
+        if rc:
+            self._chk(rc, w)
         return out
 
     # -- status -------------------------------------------------------------------------

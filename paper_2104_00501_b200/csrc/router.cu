@@ -542,7 +542,8 @@ bool route_sizes(int type, uint64_t stride, uint64_t n, uint32_t experts, uint32
 extern "C" nups_status nups_route_scratch(nups_store* s, uint64_t n, uint32_t experts, uint64_t* h_bytes_out)
 {
     if (!s || !h_bytes_out || experts < 1 || experts > NUPS_ROUTE_MAX_EXPERTS || n >= (1ull << 32)) return NUPS_EINVAL;
-    *h_bytes_out = (uint64_t)route_blocks(s, n, experts) * (experts + 1) * 8;
+    const uint64_t blocks = route_blocks(s, n, experts);
+    *h_bytes_out = blocks > 1 ? blocks * (experts + 1) * 8 : 0;           // one block finishes by itself
     return NUPS_OK;
 }
 
@@ -555,7 +556,7 @@ extern "C" nups_status nups_route(nups_store* s, const void* d_logits, int type,
     if (n && (!d_logits || !d_choice || !d_weight)) return NUPS_EINVAL;
     uint64_t bytes = 0;
     nups_route_scratch(s, n, experts, &bytes);
-    if (n && (!d_scratch || scratch_bytes < bytes || ((uintptr_t)d_scratch & 255))) return NUPS_EINVAL;
+    if (bytes && (!d_scratch || scratch_bytes < bytes || ((uintptr_t)d_scratch & 255))) return NUPS_EINVAL;
     nups_status rc = on_own_device(s);
     if (rc != NUPS_OK) return rc;
     cudaStream_t st = (cudaStream_t)stream;

@@ -200,7 +200,7 @@ def test_no_items_and_none_that_takes_part(store):
 
 def test_a_program_that_only_answers(store):
     x = make(100, 60, BF16, 11)
-    full, short = store.route(x, 4, renormalize=True), store.route(x, 4, renormalize=True, losses=False)
+    full, short = store.route(x, 4, renormalize=True, losses=True), store.route(x, 4, renormalize=True)
     assert short.prob is None and short.loss is None and short.lse is None
     for a, b in ((full.choice, short.choice), (full.weight, short.weight), (full.counts, short.counts), (full.tokens, short.tokens)):
         assert torch.equal(a, b)
@@ -297,8 +297,8 @@ def test_refusals(store):
     refused(E, lambda: store.route(x, 2, active=torch.ones(8, device="cuda")))
     refused(E, lambda: store.route(x, 2, balance=float("nan")))
     refused(E, lambda: store.route(x.cpu(), 2))
-    r = store.route(x, 2)
-    refused(E, lambda: store.route_grad(x, store.route(x, 2, losses=False)))
+    r = store.route(x, 2, losses=True)
+    refused(E, lambda: store.route_grad(x, store.route(x, 2)))
     refused(E, lambda: store.route_grad(x[:7], r))
     refused(E, lambda: store.route_grad(x[:, :39], r))
     refused(E, lambda: store.route_grad(x, r, dweight=torch.ones((8, 3), device="cuda")))
@@ -307,10 +307,12 @@ def test_refusals(store):
     refused(E, lambda: store.route_grad(x, r, out=x.half()))
     L, p = store._l, (lambda t: t.data_ptr())
     small = torch.empty(256, dtype=torch.uint8, device="cuda")
+    x = make(80, 40, F32, 15)                               # more than one block's items
+    r = store.route(x, 2)
     kept = [torch.full_like(t, 7) for t in (r.choice, r.weight, r.counts, r.tokens)]
     for address, size in ((p(small), 8), (None, 1 << 20), (p(small) + 4, 1 << 20)):
-        assert L.nups_route(store._s, p(x), 0, 40, 8, 40, 2, None, 0, 0.0, 0.0, p(kept[0]), p(kept[1]), None, p(kept[2]), p(kept[3]), None, None, address, size, None) == E
-    assert L.nups_route(store._s, p(x), 0, 39, 8, 40, 2, None, 0, 0.0, 0.0, p(kept[0]), p(kept[1]), None, p(kept[2]), p(kept[3]), None, None, p(small), 1 << 20, None) == E
+        assert L.nups_route(store._s, p(x), 0, 40, 80, 40, 2, None, 0, 0.0, 0.0, p(kept[0]), p(kept[1]), None, p(kept[2]), p(kept[3]), None, None, address, size, None) == E
+    assert L.nups_route(store._s, p(x), 0, 39, 80, 40, 2, None, 0, 0.0, 0.0, p(kept[0]), p(kept[1]), None, p(kept[2]), p(kept[3]), None, None, p(small), 1 << 20, None) == E
     torch.cuda.synchronize()
     assert all((t == 7).all() for t in kept)
 
