@@ -1,10 +1,11 @@
 // Layer norm of dense rows and of pulled rows, and its backward pass.
 //
 // y = (x - mean) rstd w + b is bound by memory: x is read once, y written once, some eight operations a value.  A row is held in
-// the registers of a team of TPR threads (EPT values each), so the variance is taken about the mean in a second pass over
-// registers, not as a difference of sums; w and b stay in registers while a team walks its rows.  Teams of up to 32 threads
-// reduce by shuffles; a block that is one team merges its warps' (sum, sum of squares about the warp's own mean) with one
-// barrier per row (Chan's formula for the variance of a union).
+// the registers of a team of TPR threads (CH chunks of VEC values each), so the variance is taken about the mean in a second pass
+// over registers, not as a difference of sums; w and b stay in registers while a team walks its rows.  A team works on ROWS rows
+// at a time: their loads are in flight together and their reductions overlap.  Teams of up to 32 threads reduce by shuffles; a
+// block that is one team merges its warps' (sum, sum of squares about the warp's own mean) with one barrier per ROWS rows (Chan's
+// formula for the variance of a union).
 #include "nups_types.cuh"
 
 namespace {
@@ -52,6 +53,14 @@ __device__ __forceinline__ void load_params(const void* p, int type, int vec, ui
     }
 }
 
+// The VEC parameters from value `at` on.
+template <class X, class A, int VEC>
+__device__ __forceinline__ void load_params_at(const void* p, int type, int vec, uint32_t at, A fill, A (&out)[1][VEC])
+{
+    const size_t size = sizeof(X) == 2 && type == NUPS_F32 ? 4 : sizeof(X);
+    load_params<X, A, VEC, 1, 1>(p ? (const char*)p + (size_t)at * size : nullptr, type, vec, VEC, 0, fill, out);
+}
+
 // One chunk of an output whose type is X, or for fp32 X also a 16-bit type.
 template <class X, class A, int VEC>
 __device__ __forceinline__ void store_chunk(void* p, int type, uint64_t at, const A* v)
@@ -91,19 +100,26 @@ __host__ __device__ constexpr int team_block(int tpr) { return tpr > 32 ? tpr : 
 // ---------------------------------------------------------------------------------------------
 // forward
 // ---------------------------------------------------------------------------------------------
-// Mean and reciprocal deviation of the row that the team holds in x (zero beyond len).
-template <class A, int VEC, int TPR, int CH>
-__device__ __forceinline__ void row_stats(const A (&x)[CH][VEC], uint32_t len, A eps, int t, int turn, A* shared, A& mean, A& rstd)
+// Mean and reciprocal deviation of the rows that the team holds (raw values; zero beyond len).
+template <class X, class A, int VEC, int TPR, int CH, int ROWS>
+__device__ __forceinline__ void row_stats(const Pack<X, VEC> (&x)[ROWS][CH], uint32_t len, A eps, int t, int turn, A* shared, A (&mean)[ROWS], A (&rstd)[ROWS])
 {
-    constexpr int WARPS = TPR / 32;
-    A sum = 0;
+    constexpr int WARPS = TPR / 32, LANES = TPR < 32 ? TPR : 32;
+    A sum[ROWS], sq[ROWS];
 #pragma unroll
-    for (int c = 0; c < CH; ++c)
+    for (int k = 0; k < ROWS; ++k) {
+        A acc[2] = {0, 0};
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) sum += x[c][j];
-    sum = team_sum<(TPR < 32 ? TPR : 32)>(sum);
-    A about;                                               // the mean that the squares are taken about: the team's, or the warp's
-    uint32_t held = len;
+        for (int c = 0; c < CH; ++c) {
+            A v[VEC];
+            unpack<A>(x[k][c], v);
+            sum_run<VEC>(acc, v);
+        }
+        sum[k] = acc[0] + acc[1];
+    }
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k) sum[k] = team_sum<LANES>(sum[k]);
+    uint32_t held = len;                                    // values of the row that the warp holds; the squares are taken about their mean
     if (TPR > 32) {
         held = 0;
 #pragma unroll
@@ -111,109 +127,160 @@ __device__ __forceinline__ void row_stats(const A (&x)[CH][VEC], uint32_t len, A
             const uint32_t at = value_at<TPR, VEC>(c, t & ~31);
             held += at < len ? min((uint32_t)(32 * VEC), len - at) : 0u;
         }
-        about = held ? sum / (A)held : (A)0;
-    } else {
-        about = sum / (A)len;
     }
-    A sq = 0;
+    const A inv_held = held ? (A)1 / (A)held : (A)0;
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-        if (value_at<TPR, VEC>(c, t) < len)
+    for (int k = 0; k < ROWS; ++k) {
+        mean[k] = TPR > 32 ? sum[k] * inv_held : sum[k] / (A)len;
+        const A minus = -mean[k];
+        A acc[2] = {0, 0};
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) { const A d = x[c][j] - about; sq += d * d; }
+        for (int c = 0; c < CH; ++c)
+            if (value_at<TPR, VEC>(c, t) < len) {
+                A v[VEC];
+                unpack<A>(x[k][c], v);
+                run_add<VEC, true>(v, v, &minus);
+                sum_run_of_products<VEC>(acc, v, v);
+            }
+        sq[k] = acc[0] + acc[1];
     }
-    sq = team_sum<(TPR < 32 ? TPR : 32)>(sq);
-    if (TPR <= 32) {
-        mean = about;
-    } else {
-        A* st = shared + (turn & 1) * 3 * WARPS;           // two sets: the next row's is written while this one is still read
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k) sq[k] = team_sum<LANES>(sq[k]);
+    if (TPR > 32) {
+        // lanes [k WARPS, (k + 1) WARPS) take row k's warps; 32 / WARPS rows at a time
+        constexpr int AT_ONCE = 32 / (WARPS > 0 ? WARPS : 1) < ROWS ? 32 / (WARPS > 0 ? WARPS : 1) : ROWS;
+        A* st = shared + (turn & 1) * (2 * ROWS + 1) * WARPS;             // two sets: the next rows' is written while this one is read
         const int warp = t >> 5, lane = t & 31;
-        if (lane == 0) { st[warp] = sum; st[WARPS + warp] = sq; st[2 * WARPS + warp] = (A)held; }
+        if (lane == 0) {
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k) { st[k * WARPS + warp] = sum[k]; st[(ROWS + k) * WARPS + warp] = sq[k]; }
+            st[2 * ROWS * WARPS + warp] = (A)held;
+        }
         __syncthreads();
-        const A s = lane < WARPS ? st[lane] : (A)0, q = lane < WARPS ? st[WARPS + lane] : (A)0, h = lane < WARPS ? st[2 * WARPS + lane] : (A)0;
-        mean = team_sum<32>(s) / (A)len;
-        const A d = h > 0 ? s / h - mean : (A)0;
-        sq = team_sum<32>(q + h * d * d);
+#pragma unroll
+        for (int k0 = 0; k0 < ROWS; k0 += AT_ONCE) {
+            const int k = k0 + (lane / (WARPS > 0 ? WARPS : 1)) % AT_ONCE, w = lane % (WARPS > 0 ? WARPS : 1);
+            const A s = st[k * WARPS + w], q = st[(ROWS + k) * WARPS + w], h = st[2 * ROWS * WARPS + w];
+            const A m = team_sum<WARPS>(s) / (A)len;
+            const A d = h > 0 ? s / h - m : (A)0;
+            const A r = inv_sqrt<A>(team_sum<WARPS>(q + h * d * d) / (A)len + eps);
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; ++i) {
+                mean[k0 + i] = __shfl_sync(0xFFFFFFFFu, m, i * WARPS);
+                rstd[k0 + i] = __shfl_sync(0xFFFFFFFFu, r, i * WARPS);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) rstd[k] = inv_sqrt<A>(sq[k] / (A)len + eps);
     }
-    rstd = inv_sqrt<A>(sq / (A)len + eps);
 }
 
-template <class X, int VEC, int TPR, int EPT, bool KEYED>
+template <class X, int VEC, int TPR, int CH, int ROWS, bool KEYED>
 __global__ void __launch_bounds__(team_block(TPR)) norm_kernel(NormArgs a, View v)
 {
     typedef typename Acc<X>::type A;
-    constexpr int CH = EPT / VEC, TEAMS = team_block(TPR) / TPR;
-    __shared__ A shared[TPR > 32 ? 6 * (TPR / 32) : 1];
+    constexpr int TEAMS = team_block(TPR) / TPR;
+    constexpr bool HOLD = TPR < 1024;                       // 64 registers a thread leave no room for the parameters
+    __shared__ A shared[TPR > 32 ? 2 * (2 * ROWS + 1) * (TPR / 32) : 1];
     grid_dependency_wait();
     const int t = threadIdx.x % TPR, team = threadIdx.x / TPR;
     A w[CH][VEC], b[CH][VEC];
-    load_params<X, A, VEC, TPR, CH>(a.w, a.w_type, a.w_vec, a.len, t, (A)1, w);
-    load_params<X, A, VEC, TPR, CH>(a.b, a.w_type, a.w_vec, a.len, t, (A)0, b);
+    if (HOLD) {
+        load_params<X, A, VEC, TPR, CH>(a.w, a.w_type, a.w_vec, a.len, t, (A)1, w);
+        load_params<X, A, VEC, TPR, CH>(a.b, a.w_type, a.w_vec, a.len, t, (A)0, b);
+    }
     int turn = 0;
-    for (uint64_t base = (uint64_t)blockIdx.x * TEAMS; base < a.n; base += (uint64_t)gridDim.x * TEAMS, ++turn) {
-        const uint64_t row = base + team;
-        const bool in = row < a.n;
-        const X* src = nullptr;
-        const X* pend = nullptr;
-        if (KEYED) {
-            if (in) {
-                const uint32_t key = __ldg(a.keys + row);
-                if (key < v.num_keys) {
-                    src = (const X*)v.val + (uint64_t)key * a.len;
-                    if (key_is_hot(v, key)) {
-                        const uint32_t slot = (uint32_t)__ldg(v.slot_of + key);
-                        pend = (const X*)v.dval + ((uint64_t)worker_of_item(row, a.n, v.R) * v.Hcap + slot) * a.len;
+    for (uint64_t base = (uint64_t)blockIdx.x * (TEAMS * ROWS); base < a.n; base += (uint64_t)gridDim.x * (TEAMS * ROWS), ++turn) {
+        Pack<X, VEC> x[ROWS][CH];
+        const X* src[ROWS];
+        const X* pend[ROWS];
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) {
+            const uint64_t row = base + k * TEAMS + team;
+            src[k] = pend[k] = nullptr;
+            if (row < a.n) {
+                if (KEYED) {
+                    const uint32_t key = __ldg(a.keys + row);
+                    if (key < v.num_keys) {
+                        src[k] = (const X*)v.val + (uint64_t)key * a.len;
+                        if (key_is_hot(v, key)) {
+                            const uint32_t slot = (uint32_t)__ldg(v.slot_of + key);
+                            pend[k] = (const X*)v.dval + ((uint64_t)worker_of_item(row, a.n, v.R) * v.Hcap + slot) * a.len;
+                        }
+                        if (v.count && t == 0) {
+                            atomicAdd(v.cnt + key, 1ull);
+                            atomicAdd(pend[k] ? &v.st->hot_hits : &v.st->cold_hits, 1ull);
+                        }
+                    } else if (t == 0) {
+                        flag_bad_key(v);
                     }
-                    if (v.count && t == 0) {
-                        atomicAdd(v.cnt + key, 1ull);
-                        atomicAdd(pend ? &v.st->hot_hits : &v.st->cold_hits, 1ull);
-                    }
-                } else if (t == 0) {
-                    flag_bad_key(v);
-                }
-            }
-        } else if (in) {
-            src = (const X*)a.x + row * a.xs;
-        }
-        A x[CH][VEC];
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const uint32_t at = value_at<TPR, VEC>(c, t);
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) x[c][j] = 0;
-            if (src && at < a.len) {
-                const Pack<X, VEC> r = load_pack<X, VEC>(src + at);
-                unpack<A>(r, x[c]);
-                if (KEYED && pend) {
-                    A d[VEC];
-                    unpack<A>(load_pack<X, VEC>(pend + at), d);
-#pragma unroll
-                    for (int j = 0; j < VEC; ++j) x[c][j] += d[j];
+                } else {
+                    src[k] = (const X*)a.x + row * a.xs;
                 }
             }
         }
-        if (KEYED && a.rows && in) {
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k)
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 const uint32_t at = value_at<TPR, VEC>(c, t);
-                if (at < a.len) store_values<X, VEC>((X*)a.rows + row * a.len + at, x[c]);
+                if (src[k] && at < a.len) x[k][c] = load_pack<X, VEC>(src[k] + at);
+                else x[k][c] = Pack<X, VEC>{};
+            }
+        if constexpr (KEYED) {
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k) {
+                const uint64_t row = base + k * TEAMS + team;
+                if (pend[k])
+#pragma unroll
+                    for (int c = 0; c < CH; ++c) {
+                        const uint32_t at = value_at<TPR, VEC>(c, t);
+                        if (at < a.len) {
+                            const Pack<X, VEC> d = load_pack<X, VEC>(pend[k] + at);
+#pragma unroll
+                            for (int j = 0; j < VEC; ++j) x[k][c].v[j] += d.v[j];
+                        }
+                    }
+                if (a.rows && row < a.n)
+#pragma unroll
+                    for (int c = 0; c < CH; ++c) {
+                        const uint32_t at = value_at<TPR, VEC>(c, t);
+                        if (at < a.len) store_pack<X, VEC>((X*)a.rows + row * a.len + at, x[k][c]);
+                    }
             }
         }
-        A mean, rstd;
-        row_stats<A, VEC, TPR, CH>(x, a.len, (A)a.eps, t, turn, shared, mean, rstd);
-        if (!in) continue;
+        A mean[ROWS], rstd[ROWS];
+        row_stats<X, A, VEC, TPR, CH, ROWS>(x, a.len, (A)a.eps, t, turn, shared, mean, rstd);
         if (t == 0) {
-            if (a.mean) ((A*)a.mean)[row] = mean;
-            if (a.rstd) ((A*)a.rstd)[row] = rstd;
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k) {
+                const uint64_t row = base + k * TEAMS + team;
+                if (row < a.n) {
+                    if (a.mean) ((A*)a.mean)[row] = mean[k];
+                    if (a.rstd) ((A*)a.rstd)[row] = rstd[k];
+                }
+            }
         }
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const uint32_t at = value_at<TPR, VEC>(c, t);
             if (at < a.len) {
-                A y[VEC];
+                A wc[1][VEC], bc[1][VEC];
+                if (!HOLD) {
+                    load_params_at<X, A, VEC>(a.w, a.w_type, a.w_vec, at, (A)1, wc);
+                    load_params_at<X, A, VEC>(a.b, a.w_type, a.w_vec, at, (A)0, bc);
+                }
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) y[j] = (x[c][j] - mean) * rstd * w[c][j] + b[c][j];
-                store_chunk<X, A, VEC>(a.y, a.y_type, row * a.ys + at, y);
+                for (int k = 0; k < ROWS; ++k) {
+                    const uint64_t row = base + k * TEAMS + team;
+                    const A off = -mean[k] * rstd[k];
+                    A y[VEC];
+                    unpack<A>(x[k][c], y);
+                    run_fma<VEC, false, true, true>(y, y, &rstd[k], &off);
+                    run_fma<VEC, false, false, false>(y, y, HOLD ? w[c] : wc[0], HOLD ? b[c] : bc[0]);
+                    if (row < a.n) store_chunk<X, A, VEC>(a.y, a.y_type, row * a.ys + at, y);
+                }
             }
         }
     }
@@ -288,8 +355,8 @@ __global__ void __launch_bounds__(1024) norm_long_kernel(NormArgs a, View v)
             A x[VEC], w[1][VEC], b[1][VEC], y[VEC];
             read(at, x);
             if (KEYED && a.rows) store_values<X, VEC>((X*)a.rows + row * a.len + at, x);
-            load_params<X, A, VEC, 1, 1>(a.w ? (const char*)a.w + (size_t)at * (sizeof(X) == 2 && a.w_type == NUPS_F32 ? 4 : sizeof(X)) : nullptr, a.w_type, a.w_vec, VEC, 0, (A)1, w);
-            load_params<X, A, VEC, 1, 1>(a.b ? (const char*)a.b + (size_t)at * (sizeof(X) == 2 && a.w_type == NUPS_F32 ? 4 : sizeof(X)) : nullptr, a.w_type, a.w_vec, VEC, 0, (A)0, b);
+            load_params_at<X, A, VEC>(a.w, a.w_type, a.w_vec, at, (A)1, w);
+            load_params_at<X, A, VEC>(a.b, a.w_type, a.w_vec, at, (A)0, b);
 #pragma unroll
             for (int j = 0; j < VEC; ++j) y[j] = (x[j] - mean) * rstd * w[0][j] + b[0][j];
             store_chunk<X, A, VEC>(a.y, a.y_type, row * a.ys + at, y);
@@ -305,27 +372,44 @@ template <class... KArgs> unsigned resident_blocks(void (*kernel)(KArgs...), int
     return n > 0 ? (unsigned)n : 1u;
 }
 
+// Chunks per thread and threads per row by the number of chunks of a row; ROWS so that a thread has some 64 bytes in flight.
 template <class X, int VEC, bool KEYED>
 nups_status launch_norm(nups_store* s, const NormArgs& a, const View& v, cudaStream_t st)
 {
-    const uint32_t len = a.len;
-#define NUPS_NORM(TPR_, EPT_)                                                                                                              \
+    const uint32_t chunks = (a.len + VEC - 1) / VEC;
+#define NUPS_NORM(TPR_, CH_, ROWS_)                                                                                                        \
     {                                                                                                                                      \
-        constexpr int TEAMS = team_block(TPR_) / TPR_;                                                                                     \
-        static const unsigned resident = resident_blocks(norm_kernel<X, VEC, TPR_, EPT_, KEYED>, team_block(TPR_));                        \
-        const unsigned grid = grid_for(a.n, TEAMS, (unsigned)s->sm_count * resident);                                                      \
-        nups_launch_dependent(norm_kernel<X, VEC, TPR_, EPT_, KEYED>, grid, team_block(TPR_), 0, st, a, v);                                \
+        constexpr int PER_BLOCK = team_block(TPR_) / TPR_ * ROWS_;                                                                         \
+        static const unsigned resident = resident_blocks(norm_kernel<X, VEC, TPR_, CH_, ROWS_, KEYED>, team_block(TPR_));                  \
+        const unsigned grid = grid_for(a.n, PER_BLOCK, (unsigned)s->sm_count * resident);                                                  \
+        nups_launch_dependent(norm_kernel<X, VEC, TPR_, CH_, ROWS_, KEYED>, grid, team_block(TPR_), 0, st, a, v);                          \
     }
-    if (len <= 64) NUPS_NORM(8, 8)
-    else if (len <= 128) NUPS_NORM(8, 16)
-    else if (len <= 256) NUPS_NORM(32, 8)
-    else if (len <= 512) NUPS_NORM(32, 16)
-    else if (len <= 1024) NUPS_NORM(128, 8)
-    else if (len <= 2048) NUPS_NORM(256, 8)
-    else if (len <= 4096) NUPS_NORM(256, 16)
-    else if (len <= 8192) NUPS_NORM(512, 16)
-    else if (len <= 16384) NUPS_NORM(1024, 16)
-    else nups_launch_dependent(norm_long_kernel<X, VEC, KEYED>, grid_for(a.n, 1, (unsigned)s->sm_count * 2), 1024, 0, st, a, v);
+    if constexpr (VEC > 1) {
+        if (chunks <= 4) NUPS_NORM(4, 1, 4)
+        else if (chunks <= 8) NUPS_NORM(8, 1, 4)
+        else if (chunks <= 16) NUPS_NORM(16, 1, 4)
+        else if (chunks <= 32) NUPS_NORM(32, 1, 4)
+        else if (chunks <= 64) NUPS_NORM(32, 2, 2)
+        else if (chunks <= 128) NUPS_NORM(128, 1, 4)
+        else if (chunks <= 256) NUPS_NORM(128, 2, 4)
+        else if (chunks <= 512) NUPS_NORM(256, 2, 4)
+        else if (chunks <= 1024) NUPS_NORM(512, 2, 2)
+        else if (chunks <= 2048) NUPS_NORM(1024, 2, 1)
+        else if (chunks <= 4096) NUPS_NORM(1024, 4, 1)
+        else nups_launch_dependent(norm_long_kernel<X, VEC, KEYED>, grid_for(a.n, 1, (unsigned)s->sm_count * 2), 1024, 0, st, a, v);
+    } else {
+        if (chunks <= 32) NUPS_NORM(32, 1, 4)
+        else if (chunks <= 64) NUPS_NORM(32, 2, 4)
+        else if (chunks <= 128) NUPS_NORM(32, 4, 4)
+        else if (chunks <= 256) NUPS_NORM(32, 8, 2)
+        else if (chunks <= 512) NUPS_NORM(32, 16, 1)
+        else if (chunks <= 1024) NUPS_NORM(128, 8, 2)
+        else if (chunks <= 2048) NUPS_NORM(256, 8, 2)
+        else if (chunks <= 4096) NUPS_NORM(256, 16, 1)
+        else if (chunks <= 8192) NUPS_NORM(512, 16, 1)
+        else if (chunks <= 16384) NUPS_NORM(1024, 16, 1)
+        else nups_launch_dependent(norm_long_kernel<X, VEC, KEYED>, grid_for(a.n, 1, (unsigned)s->sm_count * 2), 1024, 0, st, a, v);
+    }
 #undef NUPS_NORM
     LAUNCH_CHECK(s);
     return NUPS_OK;
@@ -412,70 +496,135 @@ struct GradArgs {
     int dy_type, w_type, w_vec;
 };
 
-// One pass: a team holds x and dy of a row in registers and, over all of its rows, its columns' shares of dweight and dbias.
-template <class X, int VEC, int TPR, int EPT>
+// One pass: a team holds x and dy of ROWS rows in registers and, over all of its rows, its columns' shares of dweight and dbias
+// (SHARED: in shared memory, where 64 registers a thread leave no room; each thread has its own columns there).
+template <class X, class D, int VEC, int TPR, int CH, int ROWS>
 __global__ void __launch_bounds__(team_block(TPR)) norm_grad_kernel(GradArgs a)
 {
     typedef typename Acc<X>::type A;
-    constexpr int CH = EPT / VEC, BLOCK = team_block(TPR), TEAMS = BLOCK / TPR, WARPS = BLOCK / 32;
-    __shared__ A shared[TPR > 32 ? 4 * WARPS : WARPS * TPR * EPT];
+    constexpr int BLOCK = team_block(TPR), TEAMS = BLOCK / TPR, WARPS = BLOCK / 32, EPT = CH * VEC;
+    constexpr bool SHARED = TPR == 1024;
+    extern __shared__ char dynamic[];                       // SHARED: [2][len] sums
+    __shared__ A shared[TPR > 32 ? 4 * ROWS * WARPS : WARPS * TPR * EPT];
     grid_dependency_wait();
     const int t = threadIdx.x % TPR, team = threadIdx.x / TPR;
     A w[CH][VEC], dw[CH][VEC], db[CH][VEC];
-    load_params<X, A, VEC, TPR, CH>(a.w, a.w_type, a.w_vec, a.len, t, (A)1, w);
+    A* const sum_w = (A*)dynamic;
+    A* const sum_b = sum_w + (SHARED ? CH * VEC * TPR : 0);
+    if (!SHARED) load_params<X, A, VEC, TPR, CH>(a.w, a.w_type, a.w_vec, a.len, t, (A)1, w);
 #pragma unroll
     for (int c = 0; c < CH; ++c)
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) dw[c][j] = db[c][j] = 0;
-    int turn = 0;
+        for (int j = 0; j < VEC; ++j) {
+            if (SHARED) sum_w[value_at<TPR, VEC>(c, t) + j] = sum_b[value_at<TPR, VEC>(c, t) + j] = 0;
+            else dw[c][j] = db[c][j] = 0;
+        }
     const A inv_len = (A)1 / (A)a.len;
-    for (uint64_t base = (uint64_t)blockIdx.x * TEAMS; base < a.n; base += (uint64_t)gridDim.x * TEAMS, ++turn) {
-        const uint64_t row = base + team;
-        const bool in = row < a.n;
-        const A mean = in ? ((const A*)a.mean)[row] : (A)0, rstd = in ? ((const A*)a.rstd)[row] : (A)0;
-        A h[CH][VEC], g[CH][VEC];
-        A s1 = 0, s2 = 0;
+    int turn = 0;
+    for (uint64_t base = (uint64_t)blockIdx.x * (TEAMS * ROWS); base < a.n; base += (uint64_t)gridDim.x * (TEAMS * ROWS), ++turn) {
+        Pack<X, VEC> x[ROWS][CH];
+        Pack<D, VEC> dy[ROWS][CH];
+        A mean[ROWS], rstd[ROWS], s1[ROWS], s2[ROWS];
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const uint32_t at = value_at<TPR, VEC>(c, t);
+        for (int k = 0; k < ROWS; ++k) {
+            const uint64_t row = base + k * TEAMS + team;
+            const bool in = row < a.n;
+            mean[k] = in ? ((const A*)a.mean)[row] : (A)0;
+            rstd[k] = in ? ((const A*)a.rstd)[row] : (A)0;
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) h[c][j] = g[c][j] = 0;
-            if (in && at < a.len) {
-                unpack<A>(load_pack<X, VEC>((const X*)a.x + row * a.xs + at), h[c]);
-                load_chunk<X, A, VEC>(a.dy, a.dy_type, row * a.dys + at, g[c]);
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) {
-                    h[c][j] = (h[c][j] - mean) * rstd;
-                    dw[c][j] += g[c][j] * h[c][j];
-                    db[c][j] += g[c][j];
-                    g[c][j] *= w[c][j];
-                    s1 += g[c][j];
-                    s2 += g[c][j] * h[c][j];
+            for (int c = 0; c < CH; ++c) {
+                const uint32_t at = value_at<TPR, VEC>(c, t);
+                if (in && at < a.len) {
+                    x[k][c] = load_pack<X, VEC>((const X*)a.x + row * a.xs + at);
+                    dy[k][c] = load_pack<D, VEC>((const D*)a.dy + row * a.dys + at);
+                } else {
+                    x[k][c] = Pack<X, VEC>{};
+                    dy[k][c] = Pack<D, VEC>{};
                 }
             }
         }
-        if (!a.dx) continue;                                // the same for the whole grid
-        s1 = team_sum<(TPR < 32 ? TPR : 32)>(s1);
-        s2 = team_sum<(TPR < 32 ? TPR : 32)>(s2);
-        if (TPR > 32) {
-            A* st = shared + (turn & 1) * 2 * WARPS;
-            const int lane = t & 31;
-            if (lane == 0) { st[t >> 5] = s1; st[WARPS + (t >> 5)] = s2; }
-            __syncthreads();
-            s1 = team_sum<32>(lane < WARPS ? st[lane] : (A)0);
-            s2 = team_sum<32>(lane < WARPS ? st[WARPS + lane] : (A)0);
-        }
-        s1 *= inv_len;
-        s2 *= inv_len;
-        if (!in) continue;
+        A a1[ROWS][2], a2[ROWS][2];
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) a1[k][0] = a1[k][1] = a2[k][0] = a2[k][1] = 0;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const uint32_t at = value_at<TPR, VEC>(c, t);
             if (at < a.len) {
-                A d[VEC];
+                A wc[1][VEC], dwc[VEC], dbc[VEC];
+                if (SHARED) {
+                    load_params_at<X, A, VEC>(a.w, a.w_type, a.w_vec, at, (A)1, wc);
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) d[j] = (g[c][j] - s1 - h[c][j] * s2) * rstd;
-                store_values<X, VEC>((X*)a.dx + row * a.dxs + at, d);
+                    for (int j = 0; j < VEC; ++j) { dwc[j] = sum_w[at + j]; dbc[j] = sum_b[at + j]; }
+                }
+                // rows that are not there have dy = 0 and rstd = 0: they add nothing
+#pragma unroll
+                for (int k = 0; k < ROWS; ++k) {
+                    const A minus = -mean[k];
+                    A h[VEC], d[VEC];
+                    unpack<A>(x[k][c], h);
+                    unpack<A>(dy[k][c], d);
+                    run_add<VEC, true>(h, h, &minus);
+                    run_scale<VEC>(h, h, rstd[k]);
+                    run_fma<VEC, false, false, false>(SHARED ? dwc : dw[c], d, h, SHARED ? dwc : dw[c]);
+                    run_add<VEC, false>(SHARED ? dbc : db[c], SHARED ? dbc : db[c], d);
+                    run_mul<VEC>(d, d, SHARED ? wc[0] : w[c]);
+                    sum_run<VEC>(a1[k], d);
+                    sum_run_of_products<VEC>(a2[k], d, h);
+                }
+                if (SHARED)
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) { sum_w[at + j] = dwc[j]; sum_b[at + j] = dbc[j]; }
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) { s1[k] = a1[k][0] + a1[k][1]; s2[k] = a2[k][0] + a2[k][1]; }
+        if (!a.dx) continue;                                // the same for the whole grid
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) {
+            s1[k] = team_sum<(TPR < 32 ? TPR : 32)>(s1[k]);
+            s2[k] = team_sum<(TPR < 32 ? TPR : 32)>(s2[k]);
+        }
+        if (TPR > 32) {
+            A* st = shared + (turn & 1) * 2 * ROWS * WARPS;
+            const int lane = t & 31;
+            if (lane == 0)
+#pragma unroll
+                for (int k = 0; k < ROWS; ++k) { st[k * WARPS + (t >> 5)] = s1[k]; st[(ROWS + k) * WARPS + (t >> 5)] = s2[k]; }
+            __syncthreads();
+            // lanes [i WARPS, (i + 1) WARPS) take sum i of the 2 ROWS, 32 / WARPS sums at a time
+            constexpr int AT_ONCE = 32 / WARPS < 2 * ROWS ? 32 / WARPS : 2 * ROWS;
+#pragma unroll
+            for (int i0 = 0; i0 < 2 * ROWS; i0 += AT_ONCE) {
+                const A sum = team_sum<WARPS>(st[(i0 + (lane / WARPS) % AT_ONCE) * WARPS + lane % WARPS]);
+#pragma unroll
+                for (int i = 0; i < AT_ONCE; ++i) {
+                    const A r = __shfl_sync(0xFFFFFFFFu, sum, i * WARPS);
+                    if (i0 + i < ROWS) s1[i0 + i] = r;
+                    else s2[i0 + i - ROWS] = r;
+                }
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const uint32_t at = value_at<TPR, VEC>(c, t);
+            if (at < a.len) {
+                A wc[1][VEC];
+                if (SHARED) load_params_at<X, A, VEC>(a.w, a.w_type, a.w_vec, at, (A)1, wc);
+#pragma unroll
+                for (int k = 0; k < ROWS; ++k) {
+                    const uint64_t row = base + k * TEAMS + team;
+                    // rstd (g - mean(g) - h mean(g h)), the two means with the factor rstd already
+                    const A minus = -mean[k], m1 = -s1[k] * inv_len * rstd[k], m2 = -s2[k] * inv_len * rstd[k];
+                    A h[VEC], d[VEC];
+                    unpack<A>(x[k][c], h);
+                    unpack<A>(dy[k][c], d);
+                    run_add<VEC, true>(h, h, &minus);
+                    run_scale<VEC>(h, h, rstd[k]);
+                    run_mul<VEC>(d, d, SHARED ? wc[0] : w[c]);
+                    run_fma<VEC, false, true, true>(h, h, &m2, &m1);
+                    run_fma<VEC, false, true, false>(d, d, &rstd[k], h);
+                    if (row < a.n) store_values<X, VEC>((X*)a.dx + row * a.dxs + at, d);
+                }
             }
         }
     }
@@ -487,7 +636,10 @@ __global__ void __launch_bounds__(team_block(TPR)) norm_grad_kernel(GradArgs a)
             const uint32_t at = value_at<TPR, VEC>(c, t);
             if (at < a.len)
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) { out[at + j] = dw[c][j]; out[a.len + at + j] = db[c][j]; }
+                for (int j = 0; j < VEC; ++j) {
+                    out[at + j] = SHARED ? sum_w[at + j] : dw[c][j];
+                    out[a.len + at + j] = SHARED ? sum_b[at + j] : db[c][j];
+                }
         }
     } else {
         // teams of a warp by shuffles, warps through shared memory; first dweight, then dbias
@@ -529,7 +681,7 @@ __global__ void __launch_bounds__(1024) norm_grad_sums_kernel(GradArgs a, typena
             A x[VEC], g[VEC], w[1][VEC];
             unpack<A>(load_pack<X, VEC>((const X*)a.x + row * a.xs + at), x);
             load_chunk<X, A, VEC>(a.dy, a.dy_type, row * a.dys + at, g);
-            load_params<X, A, VEC, 1, 1>(a.w ? (const char*)a.w + (size_t)at * (sizeof(X) == 2 && a.w_type == NUPS_F32 ? 4 : sizeof(X)) : nullptr, a.w_type, a.w_vec, VEC, 0, (A)1, w);
+            load_params_at<X, A, VEC>(a.w, a.w_type, a.w_vec, at, (A)1, w);
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
                 const A gj = g[j] * w[0][j];
@@ -551,7 +703,7 @@ __global__ void __launch_bounds__(256) norm_grad_apply_kernel(GradArgs a, const 
     const uint32_t at = (blockIdx.x * 256 + threadIdx.x) * VEC;
     if (at >= a.len) return;
     A w[1][VEC], dw[VEC], db[VEC];
-    load_params<X, A, VEC, 1, 1>(a.w ? (const char*)a.w + (size_t)at * (sizeof(X) == 2 && a.w_type == NUPS_F32 ? 4 : sizeof(X)) : nullptr, a.w_type, a.w_vec, VEC, 0, (A)1, w);
+    load_params_at<X, A, VEC>(a.w, a.w_type, a.w_vec, at, (A)1, w);
 #pragma unroll
     for (int j = 0; j < VEC; ++j) dw[j] = db[j] = 0;
     for (uint64_t row = blockIdx.y; row < a.n; row += gridDim.y) {
@@ -599,29 +751,35 @@ __global__ void __launch_bounds__(1024) norm_grad_join_kernel(const A* part, uin
     }
 }
 
-constexpr uint32_t GRAD_LONG = 8192;       // longer rows (fp64: half of it) take two passes
-uint32_t grad_long_from(int type) { return type == NUPS_F64 ? GRAD_LONG / 2 : GRAD_LONG; }
+// The longest rows that a team holds; longer ones take two passes over x and dy.
+uint32_t grad_long_from(int type) { return type == NUPS_F64 ? 4096 : 16384; }
 
 // Blocks that leave sums: a rule on the sizes alone, so that the order of the additions is theirs too.
-uint32_t grad_teams(uint32_t len) { return len <= 128 ? 32 : len <= 512 ? 8 : 1; }
 unsigned grad_blocks(const nups_store* s, uint64_t n, uint32_t len, int type)
 {
     const unsigned sm = (unsigned)s->sm_count;
+    const uint32_t bytes = len * (uint32_t)type_bytes(type);
     if (len > grad_long_from(type)) return grid_for(n, 16, 32);
-    return grid_for(n, grad_teams(len), sm * (len <= 512 ? 4 : len <= 2048 ? 6 : len <= 4096 ? 2 : 1));
+    return grid_for(n, bytes <= 128 ? 64 : bytes <= 1024 ? 8 : 2, sm * (bytes <= 1024 ? 3 : bytes <= 4096 ? 4 : bytes <= 8192 ? 2 : 1));
 }
 uint64_t grad_part_bytes(const nups_store* s, uint64_t n, uint32_t len, int type)
 {
     return (uint64_t)grad_blocks(s, n, len, type) * 2 * len * (type == NUPS_F64 ? 8 : 4);
 }
 
-template <class X, int VEC>
+template <class X, class D, int VEC>
 nups_status launch_grad(nups_store* s, GradArgs a, int x_type, void* d_dw, void* d_db, char* scratch, cudaStream_t st)
 {
     typedef typename Acc<X>::type A;
     const uint32_t len = a.len;
     const unsigned blocks = grad_blocks(s, a.n, len, x_type);
-#define NUPS_GRAD(TPR_, EPT_) nups_launch_dependent(norm_grad_kernel<X, VEC, TPR_, EPT_>, blocks, team_block(TPR_), 0, st, a)
+    const uint32_t chunks = (len + VEC - 1) / VEC;
+#define NUPS_GRAD(TPR_, CH_, ROWS_)                                                                                       \
+    {                                                                                                                     \
+        const unsigned smem = TPR_ == 1024 ? 2 * TPR_ * CH_ * VEC * (unsigned)sizeof(A) : 0;                              \
+        if (smem > 48 * 1024) CK(cudaFuncSetAttribute(norm_grad_kernel<X, D, VEC, TPR_, CH_, ROWS_>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)); \
+        nups_launch_dependent(norm_grad_kernel<X, D, VEC, TPR_, CH_, ROWS_>, blocks, team_block(TPR_), smem, st, a);      \
+    }
     if (len > grad_long_from(x_type)) {
         A* sums = (A*)(scratch + (a.part ? (grad_part_bytes(s, a.n, len, x_type) + 255) / 256 * 256 : 0));
         if (a.dx) {
@@ -630,14 +788,30 @@ nups_status launch_grad(nups_store* s, GradArgs a, int x_type, void* d_dw, void*
         }
         nups_launch_dependent(norm_grad_apply_kernel<X, VEC>, dim3(grid_for(len, 256 * VEC), blocks), 256, 0, st, a, (const A*)sums);
     }
-    else if (len <= 64) NUPS_GRAD(8, 8);
-    else if (len <= 128) NUPS_GRAD(8, 16);
-    else if (len <= 256) NUPS_GRAD(32, 8);
-    else if (len <= 512) NUPS_GRAD(32, 16);
-    else if (len <= 1024) NUPS_GRAD(128, 8);
-    else if (len <= 2048) NUPS_GRAD(128, 16);
-    else if (len <= 4096) NUPS_GRAD(256, 16);
-    else NUPS_GRAD(512, 16);
+    else if constexpr (VEC > 1) {
+        if (chunks <= 4) NUPS_GRAD(4, 1, 4)
+        else if (chunks <= 8) NUPS_GRAD(8, 1, 4)
+        else if (chunks <= 16) NUPS_GRAD(16, 1, 4)
+        else if (chunks <= 32) NUPS_GRAD(32, 1, 4)
+        else if (chunks <= 64) NUPS_GRAD(32, 2, 2)
+        else if (chunks <= 128) NUPS_GRAD(128, 1, 4)
+        else if (chunks <= 256) NUPS_GRAD(128, 2, 2)
+        else if (chunks <= 512) NUPS_GRAD(256, 2, 2)
+        else if (chunks <= 1024) NUPS_GRAD(512, 2, 1)
+        else if (chunks <= 2048) NUPS_GRAD(1024, 2, 1)
+        else if constexpr (VEC == 4) NUPS_GRAD(1024, 4, 1)
+    } else {
+        if (chunks <= 32) NUPS_GRAD(32, 1, 4)
+        else if (chunks <= 64) NUPS_GRAD(32, 2, 4)
+        else if (chunks <= 128) NUPS_GRAD(32, 4, 2)
+        else if (chunks <= 256) NUPS_GRAD(32, 8, 1)
+        else if (chunks <= 512) NUPS_GRAD(32, 16, 1)
+        else if (chunks <= 1024) NUPS_GRAD(128, 8, 1)
+        else if (chunks <= 2048) NUPS_GRAD(128, 16, 1)
+        else if (chunks <= 4096) NUPS_GRAD(256, 16, 1)
+        else if (sizeof(A) == 4 && chunks <= 8192) NUPS_GRAD(512, 16, 1)
+        else if constexpr (sizeof(A) == 4) NUPS_GRAD(1024, 16, 1)
+    }
 #undef NUPS_GRAD
     LAUNCH_CHECK(s);
     if (a.part) {
@@ -690,10 +864,12 @@ extern "C" nups_status nups_layer_norm_grad(nups_store* s, const void* d_x, int 
     const size_t run = (size_t)vec * (w_type == NUPS_F32 && x_type != NUPS_F64 ? 4 : type_bytes(x_type));
     a.w_vec = wide && aligned(d_weight, run > 16 ? 16 : run);
     char* scratch = (char*)d_scratch;
+#define NUPS_LAUNCH(X_, D_, V_) (wide ? launch_grad<X_, D_, V_>(s, a, x_type, d_dweight, d_dbias, scratch, st) : launch_grad<X_, D_, 1>(s, a, x_type, d_dweight, d_dbias, scratch, st))
     switch (x_type) {
-        case NUPS_F64: return wide ? launch_grad<double, 2>(s, a, x_type, d_dweight, d_dbias, scratch, st) : launch_grad<double, 1>(s, a, x_type, d_dweight, d_dbias, scratch, st);
-        case NUPS_F32: return wide ? launch_grad<float, 4>(s, a, x_type, d_dweight, d_dbias, scratch, st) : launch_grad<float, 1>(s, a, x_type, d_dweight, d_dbias, scratch, st);
-        case NUPS_F16: return wide ? launch_grad<__half, 8>(s, a, x_type, d_dweight, d_dbias, scratch, st) : launch_grad<__half, 1>(s, a, x_type, d_dweight, d_dbias, scratch, st);
-        default: return wide ? launch_grad<__nv_bfloat16, 8>(s, a, x_type, d_dweight, d_dbias, scratch, st) : launch_grad<__nv_bfloat16, 1>(s, a, x_type, d_dweight, d_dbias, scratch, st);
+        case NUPS_F64: return NUPS_LAUNCH(double, double, 2);
+        case NUPS_F32: return dy_type == NUPS_F32 ? NUPS_LAUNCH(float, float, 4) : dy_type == NUPS_F16 ? NUPS_LAUNCH(float, __half, 4) : NUPS_LAUNCH(float, __nv_bfloat16, 4);
+        case NUPS_F16: return NUPS_LAUNCH(__half, __half, 8);
+        default: return NUPS_LAUNCH(__nv_bfloat16, __nv_bfloat16, 8);
     }
+#undef NUPS_LAUNCH
 }
