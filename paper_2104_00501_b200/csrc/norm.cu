@@ -6,6 +6,9 @@
 // at a time: their loads are in flight together and their reductions overlap.  Teams of up to 32 threads reduce by shuffles; a
 // block that is one team merges its warps' (sum, sum of squares about the warp's own mean) with one barrier per ROWS rows (Chan's
 // formula for the variance of a union).
+#include <atomic>
+
+#include "nups_tcgen05.cuh"
 #include "nups_types.cuh"
 
 namespace {
@@ -23,6 +26,7 @@ struct NormArgs {
     double eps;
     const uint32_t* keys;      // pull_norm: rows come from the store
     void* rows;
+    DevStat* st;
 };
 
 // Values that thread t of a team of TPR holds: chunk c covers VEC values from (c * TPR + t) * VEC.
@@ -100,9 +104,10 @@ __host__ __device__ constexpr int team_block(int tpr) { return tpr > 32 ? tpr : 
 // ---------------------------------------------------------------------------------------------
 // forward
 // ---------------------------------------------------------------------------------------------
-// Mean and reciprocal deviation of the rows that the team holds (raw values; zero beyond len).
-template <class X, class A, int VEC, int TPR, int CH, int ROWS>
-__device__ __forceinline__ void row_stats(const Pack<X, VEC> (&x)[ROWS][CH], uint32_t len, A eps, int t, int turn, A* shared, A (&mean)[ROWS], A (&rstd)[ROWS])
+// Mean and reciprocal deviation of ROWS rows; x(k, c, v) gives the thread's chunk c of row k (zero beyond len), sync() is the barrier
+// of a block that is one team.
+template <class A, int VEC, int TPR, int CH, int ROWS, class Get, class Sync>
+__device__ __forceinline__ void row_stats(Get x, Sync sync, uint32_t len, A eps, int t, int turn, A* shared, A (&mean)[ROWS], A (&rstd)[ROWS])
 {
     constexpr int WARPS = TPR / 32, LANES = TPR < 32 ? TPR : 32;
     A sum[ROWS], sq[ROWS];
@@ -112,7 +117,7 @@ __device__ __forceinline__ void row_stats(const Pack<X, VEC> (&x)[ROWS][CH], uin
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             A v[VEC];
-            unpack<A>(x[k][c], v);
+            x(k, c, v);
             sum_run<VEC>(acc, v);
         }
         sum[k] = acc[0] + acc[1];
@@ -138,7 +143,7 @@ __device__ __forceinline__ void row_stats(const Pack<X, VEC> (&x)[ROWS][CH], uin
         for (int c = 0; c < CH; ++c)
             if (value_at<TPR, VEC>(c, t) < len) {
                 A v[VEC];
-                unpack<A>(x[k][c], v);
+                x(k, c, v);
                 run_add<VEC, true>(v, v, &minus);
                 sum_run_of_products<VEC>(acc, v, v);
             }
@@ -156,7 +161,7 @@ __device__ __forceinline__ void row_stats(const Pack<X, VEC> (&x)[ROWS][CH], uin
             for (int k = 0; k < ROWS; ++k) { st[k * WARPS + warp] = sum[k]; st[(ROWS + k) * WARPS + warp] = sq[k]; }
             st[2 * ROWS * WARPS + warp] = (A)held;
         }
-        __syncthreads();
+        sync();
 #pragma unroll
         for (int k0 = 0; k0 < ROWS; k0 += AT_ONCE) {
             const int k = k0 + (lane / (WARPS > 0 ? WARPS : 1)) % AT_ONCE, w = lane % (WARPS > 0 ? WARPS : 1);
@@ -251,7 +256,7 @@ __global__ void __launch_bounds__(team_block(TPR)) norm_kernel(NormArgs a, View 
             }
         }
         A mean[ROWS], rstd[ROWS];
-        row_stats<X, A, VEC, TPR, CH, ROWS>(x, a.len, (A)a.eps, t, turn, shared, mean, rstd);
+        row_stats<A, VEC, TPR, CH, ROWS>([&](int k, int c, A* to) { unpack<A>(x[k][c], to); }, [] { __syncthreads(); }, a.len, (A)a.eps, t, turn, shared, mean, rstd);
         if (t == 0) {
 #pragma unroll
             for (int k = 0; k < ROWS; ++k) {
@@ -283,6 +288,99 @@ __global__ void __launch_bounds__(team_block(TPR)) norm_kernel(NormArgs a, View 
                 }
             }
         }
+    }
+}
+
+// Rows of 1 KB and more: the rows come into a ring of STAGES groups of ROWS rows in shared memory by bulk copies, a group or two ahead
+// of the arithmetic, which reads them there three times; what is in flight takes no registers and does not stop at the block's barrier.
+// (16,384 rows of 4096 bf16: 55 us with the rows in registers, two blocks of 256 threads per multiprocessor.)
+template <class X, int TPR, int CH, int ROWS, int STAGES>
+__global__ void __launch_bounds__(TPR) norm_ring_kernel(NormArgs a)
+{
+    typedef typename Acc<X>::type A;
+    constexpr int VEC = 16 / sizeof(X);
+    constexpr bool HOLD = CH * VEC * TPR * sizeof(A) <= 32768;            // up to 32 registers of parameters where a thread may have them
+    extern __shared__ __align__(128) char ring[];
+    __shared__ A shared[2 * (2 * ROWS + 1) * (TPR / 32)];
+    __shared__ uint64_t bars[STAGES];
+    const int t = threadIdx.x;
+    const uint32_t bytes = a.len * sizeof(X), stage_bytes = bytes * ROWS;
+    const uint64_t step = (uint64_t)gridDim.x * ROWS, first = (uint64_t)blockIdx.x * ROWS;
+    auto bar = [&](uint32_t s) { return smem_address(&bars[s]); };
+    if (t == 0) {
+        for (int s = 0; s < STAGES; ++s) mbar_init(bar(s), 1);
+        mbar_init_visible();
+    }
+    grid_dependency_wait();
+    auto issue = [&](uint32_t i) {                          // the block's group i; one thread
+        const uint64_t base = first + i * step;
+        if (base >= a.n) return;
+        const uint32_t rows = (uint32_t)min((uint64_t)ROWS, a.n - base), s = i % STAGES, to = smem_address(ring) + s * stage_bytes;
+        mbar_expect(bar(s), rows * bytes);
+        if (a.xs == a.len) bulk_load(to, (const X*)a.x + base * a.xs, rows * bytes, bar(s));
+        else
+            for (uint32_t k = 0; k < rows; ++k) bulk_load(to + k * bytes, (const X*)a.x + (base + k) * a.xs, bytes, bar(s));
+    };
+    if (t == 0)
+        for (uint32_t i = 0; i + 1 < STAGES; ++i) issue(i);
+    A w[CH][VEC], b[CH][VEC];
+    if (HOLD) {
+        load_params<X, A, VEC, TPR, CH>(a.w, a.w_type, a.w_vec, a.len, t, (A)1, w);
+        load_params<X, A, VEC, TPR, CH>(a.b, a.w_type, a.w_vec, a.len, t, (A)0, b);
+    }
+    __syncthreads();                                        // the barriers are there
+    uint32_t i = 0;
+    bool ok = true;
+    for (uint64_t base = first; base < a.n; base += step, ++i) {
+        const uint32_t s = i % STAGES;
+        const X* x = (const X*)(ring + s * stage_bytes);
+        ok = mbar_wait(bar(s), (i / STAGES) & 1);
+        bool stop = false;
+        auto get = [&](int k, int c, A* to) {
+            const uint32_t at = value_at<TPR, VEC>(c, t);
+            if (at < a.len) unpack<A>(load_pack<X, VEC>(x + k * a.len + at), to);
+            else
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) to[j] = 0;
+        };
+        A mean[ROWS], rstd[ROWS];
+        row_stats<A, VEC, TPR, CH, ROWS>(get, [&] { stop = __syncthreads_or(!ok); }, a.len, (A)a.eps, t, (int)i, shared, mean, rstd);
+        if (stop) { ok = false; break; }
+        if (t == 0) {                                       // every thread is done with the group before this one
+            issue(i + STAGES - 1);
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k)
+                if (base + k < a.n) {
+                    if (a.mean) ((A*)a.mean)[base + k] = mean[k];
+                    if (a.rstd) ((A*)a.rstd)[base + k] = rstd[k];
+                }
+        }
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const uint32_t at = value_at<TPR, VEC>(c, t);
+            if (at < a.len) {
+                A wc[1][VEC], bc[1][VEC];
+                if (!HOLD) {
+                    load_params_at<X, A, VEC>(a.w, a.w_type, a.w_vec, at, (A)1, wc);
+                    load_params_at<X, A, VEC>(a.b, a.w_type, a.w_vec, at, (A)0, bc);
+                }
+#pragma unroll
+                for (int k = 0; k < ROWS; ++k) {
+                    const A off = -mean[k] * rstd[k];
+                    A y[VEC];
+                    get(k, c, y);
+                    run_fma<VEC, false, true, true>(y, y, &rstd[k], &off);
+                    run_fma<VEC, false, false, false>(y, y, HOLD ? w[c] : wc[0], HOLD ? b[c] : bc[0]);
+                    if (base + k < a.n) store_chunk<X, A, VEC>(a.y, a.y_type, (base + k) * a.ys + at, y);
+                }
+            }
+        }
+    }
+    if (!ok) {                                              // a copy did not come: say so, and leave none in flight
+        atomicCAS(&a.st->status, 0, NUPS_ETIMEOUT);
+        if (t == 0)
+            for (uint32_t k = i + 1; k < i + STAGES - 1; ++k)
+                if (first + k * step < a.n) mbar_wait(bar(k % STAGES), (k / STAGES) & 1);
     }
 }
 
@@ -372,11 +470,46 @@ template <class... KArgs> unsigned resident_blocks(void (*kernel)(KArgs...), int
     return n > 0 ? (unsigned)n : 1u;
 }
 
+// The same with dynamic shared memory, whose size the call decides; also asks for that much on the device.  What the last call with
+// this kernel found is remembered (device, size, blocks): the two queries take a microsecond.
+template <class... KArgs> unsigned ring_blocks(std::atomic<uint64_t>& last, int device, void (*kernel)(KArgs...), int block, size_t smem)
+{
+    const uint64_t key = ((uint64_t)(device + 1) << 48) | ((uint64_t)smem << 16), seen = last.load(std::memory_order_relaxed);
+    if ((seen & ~0xFFFFull) == key) return (unsigned)(seen & 0xFFFF);
+    int n = 0;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return 0;
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, block, smem) != cudaSuccess || n < 1) return 0;
+    last.store(key | (uint64_t)n, std::memory_order_relaxed);
+    return (unsigned)n;
+}
+
 // Chunks per thread and threads per row by the number of chunks of a row; ROWS so that a thread has some 64 bytes in flight.
 template <class X, int VEC, bool KEYED>
 nups_status launch_norm(nups_store* s, const NormArgs& a, const View& v, cudaStream_t st)
 {
     const uint32_t chunks = (a.len + VEC - 1) / VEC;
+#define NUPS_RING(TPR_, CH_, ROWS_, STAGES_)                                                                                               \
+    {                                                                                                                                      \
+        const size_t smem = (size_t)STAGES_ * ROWS_ * a.len * sizeof(X);                                                                   \
+        static std::atomic<uint64_t> last{0};                                                                                              \
+        const unsigned resident = ring_blocks(last, s->device, norm_ring_kernel<X, TPR_, CH_, ROWS_, STAGES_>, TPR_, smem);                \
+        if (!resident) return nups_cuda_fail(cudaGetLastError(), "norm_ring_kernel");                                                      \
+        const unsigned grid = grid_for(a.n, ROWS_, (unsigned)s->sm_count * resident);                                                      \
+        nups_launch_dependent(norm_ring_kernel<X, TPR_, CH_, ROWS_, STAGES_>, grid, TPR_, smem, st, a);                                    \
+        LAUNCH_CHECK(s);                                                                                                                   \
+        return NUPS_OK;                                                                                                                    \
+    }
+    if constexpr (VEC > 1 && !KEYED) {
+        if (chunks > 64 && a.n > (uint64_t)s->sm_count) {   // fewer rows: every block has one group, nothing to run ahead of
+            if (chunks <= 128) NUPS_RING(128, 1, 4, 3)
+            if (chunks <= 256) NUPS_RING(128, 2, 4, 3)
+            if (chunks <= 512) NUPS_RING(256, 2, 4, 2)
+            if (chunks <= 1024) NUPS_RING(512, 2, 2, 3)
+            if (chunks <= 2048) NUPS_RING(1024, 2, 2, 3)
+            if (chunks <= 4096) NUPS_RING(1024, 4, 1, 3)
+        }
+    }
+#undef NUPS_RING
 #define NUPS_NORM(TPR_, CH_, ROWS_)                                                                                                        \
     {                                                                                                                                      \
         constexpr int PER_BLOCK = team_block(TPR_) / TPR_ * ROWS_;                                                                         \
@@ -448,7 +581,7 @@ extern "C" nups_status nups_layer_norm(nups_store* s, const void* d_x, int x_typ
     if (n && (!d_x || !d_y)) return NUPS_EINVAL;
     nups_status rc = on_own_device(s);
     if (rc != NUPS_OK || n == 0) return rc;
-    NormArgs a = {d_x, x_stride, d_y, y_stride, d_weight, d_bias, d_mean, d_rstd, n, len, y_type, w_type, 0, eps, nullptr, nullptr};
+    NormArgs a = {d_x, x_stride, d_y, y_stride, d_weight, d_bias, d_mean, d_rstd, n, len, y_type, w_type, 0, eps, nullptr, nullptr, s->st};
     const View v = {};
     cudaStream_t st = (cudaStream_t)stream;
     const int vec = (int)(16 / type_bytes(x_type));
@@ -471,7 +604,7 @@ extern "C" nups_status nups_pull_norm(nups_store* s, const uint32_t* d_keys, uin
     if (!aligned(d_y, 16) || !aligned(d_rows, 16)) return NUPS_EINVAL;
     nups_status rc = on_own_device(s);
     if (rc != NUPS_OK || n == 0) return rc;
-    NormArgs a = {s->val, s->value_len, d_y, s->value_len, d_weight, d_bias, d_mean, d_rstd, n, s->value_len, y_type, type, 0, eps, d_keys, d_rows};
+    NormArgs a = {s->val, s->value_len, d_y, s->value_len, d_weight, d_bias, d_mean, d_rstd, n, s->value_len, y_type, type, 0, eps, d_keys, d_rows, s->st};
     a.w_vec = params_vec(a, type, type == NUPS_F64 ? 2 : 4);
     const View v = nups_view(s);
     return type == NUPS_F64 ? launch_norm<double, 2, true>(s, a, v, (cudaStream_t)stream) : launch_norm<float, 4, true>(s, a, v, (cudaStream_t)stream);

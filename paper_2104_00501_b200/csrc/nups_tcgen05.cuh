@@ -44,6 +44,11 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity)
     return true;
 }
 
+// A contiguous run; both addresses 16-byte aligned, its size a multiple of 16.
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
 // One box of a three-dimensional tensor map; x in elements of the innermost dimension, its bytes a multiple of 16.
 __device__ __forceinline__ void tma_load(uint32_t dst, const void* map, int x, int y, int z, uint32_t bar)
 {

@@ -342,9 +342,11 @@ __global__ void __launch_bounds__(256) orth_split_kernel(OrthArgs a, Planes p)
 }
 
 enum { GRAM = 0, POLYNOMIAL = 1, PRODUCT = 2, LAST = 3, PART = 4 };
-constexpr int BLOCK_M = 128, PAIR_M = 256, TILE_N = 128, TILE_K = 64, STAGES = 2, TILED_BLOCK = 320, SUM_WARPS = 8;
-constexpr uint32_t A_BYTES = BLOCK_M * TILE_K * 2, B_BYTES = TILE_N / 2 * TILE_K * 2, STAGE_BYTES = 2 * (A_BYTES + B_BYTES);
-constexpr uint32_t TILED_SMEM = STAGES * STAGE_BYTES + 1024;
+constexpr int BLOCK_M = 128, PAIR_M = 256, TILE_K = 64, TILED_BLOCK = 320, SUM_WARPS = 8;
+constexpr uint32_t A_BYTES = BLOCK_M * TILE_K * 2, BOX64_BYTES = 64 * TILE_K * 2;
+// One block per multiprocessor, and nothing beside it: two pairs that ask for tensor memory on the same two multiprocessors at
+// the same time could each hold the right to allocate on one of them and wait for it on the other.
+constexpr uint32_t TILED_SMEM = 192 * 1024 + 1024;
 
 struct TiledArgs {
     uint32_t m, n, k_blocks;   // rows and columns of the result, runs of TILE_K values of K
@@ -366,7 +368,7 @@ __device__ __forceinline__ bool group_all(uint32_t group, bool ok)
 }
 
 // How many tiles of the 256 rows bi of a symmetric result reach the diagonal or lie below it.
-__host__ __device__ constexpr uint32_t tiles_of_rows(uint32_t bi) { return (PAIR_M / TILE_N) * (bi + 1); }
+__host__ __device__ constexpr uint32_t tiles_of_rows(uint32_t bi, uint32_t tile_n) { return (PAIR_M / tile_n) * (bi + 1); }
 
 // 32 results of each of a warp's 32 rows (one row per lane) to a row-major matrix, through shared memory so that a store covers
 // one row.  at: the first row's first value.
@@ -381,21 +383,23 @@ __device__ __forceinline__ void write_rows(void* out, int type, uint64_t at, uin
         for (uint32_t r = 0; r < min(rows, 32u); ++r) write_value(out, type, at + r * stride + lane, tile[r * 33 + lane]);
 }
 
-// A tile of 256 x 128 results by a pair of blocks, 128 rows each.  In each block warp 0 brings in the operands' pairs by TMA; warp 1
+// A tile of 256 x TILE_N results (128 or 256) by a pair of blocks, 128 rows each.  In each block warp 0 brings in the operands' pairs by TMA; warp 1
 // of the first block issues the products of both (cta_group::2: each block reads its own rows of A and half of B, so shared
 // memory is read and filled at two thirds of the rate that a block on its own would need); eight warps sum.  The tensor cores cut
 // what an addition shifts out, so a long sum in tensor memory drifts towards zero (1e-6 of a 1024-term sum, which the iteration
 // multiplies: 1e-4 of the result at 4096 x 4096).  Each run of TILE_K values of K therefore starts anew in one of two sets of
 // accumulators, the small products hi lo and lo hi first, and is added in registers, with rounding, while the next run is
-// multiplied.  Two blocks share a multiprocessor: one's products hide the other's start and end.
+// multiplied.
 // The result leaves through shared memory in the operands' layout, by TMA; below the diagonal a second, transposed time.
-template <int MODE>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TILED_BLOCK, 2)
+template <int MODE, int TILE_N>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TILED_BLOCK, 1)
 orth_tiled_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_old,
                   const __grid_constant__ CUtensorMap map_to, const __grid_constant__ CUtensorMap map_mirror, TiledArgs t, OrthArgs o)
 {
     constexpr bool SYMMETRIC = MODE == GRAM || MODE == POLYNOMIAL || MODE == PART, MN_MAJOR = !SYMMETRIC;
-    constexpr int OWN = TILE_N / 2;                         // columns that a summing warp takes
+    constexpr int OWN = TILE_N / 2, PANELS = OWN / 64;      // columns that a summing warp takes
+    constexpr uint32_t B_BYTES = TILE_N / 2 * TILE_K * 2, STAGE_BYTES = 2 * (A_BYTES + B_BYTES), STAGES = TILE_N == 256 ? 3 : 4;
+    static_assert(STAGES * STAGE_BYTES + 1024 == TILED_SMEM && 4 * PANELS * PANEL <= STAGES * STAGE_BYTES, "shared memory of a block");
     extern __shared__ char raw[];
     __shared__ uint64_t bars[3 * STAGES + 5];
     __shared__ uint32_t tmem_mem;
@@ -404,7 +408,7 @@ orth_tiled_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     const uint32_t rank = blockIdx.x & 1;
     uint32_t bi = 0, bj = blockIdx.x >> 1;
     if (SYMMETRIC) {
-        while (bj >= tiles_of_rows(bi)) bj -= tiles_of_rows(bi++);
+        while (bj >= tiles_of_rows(bi, TILE_N)) bj -= tiles_of_rows(bi++, TILE_N);
     } else {
         bi = bj / t.tiles_n;
         bj -= bi * t.tiles_n;
@@ -422,7 +426,7 @@ orth_tiled_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     auto ready = [&](uint32_t b) { return smem_address(&bars[3 * STAGES + 2 + b]); };    // ... is complete
     const uint32_t old_here = smem_address(&bars[3 * STAGES + 4]);
     if (threadIdx.x == 0) {
-        for (int s = 0; s < STAGES; ++s) { mbar_init(full(s), 1); mbar_init(other(s), 1); mbar_init(empty(s), 1); }
+        for (uint32_t s = 0; s < STAGES; ++s) { mbar_init(full(s), 1); mbar_init(other(s), 1); mbar_init(empty(s), 1); }
         for (int b = 0; b < 2; ++b) { mbar_init(summed(b), 2 * SUM_WARPS); mbar_init(ready(b), 1); }
         mbar_init(old_here, 1);
         mbar_init_visible();
@@ -452,7 +456,13 @@ orth_tiled_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
 #pragma unroll
                 for (int p = 0; p < 2; ++p) {
                     tma_load(to + p * A_BYTES, &map_a, k0, (int)row0, z + p, full(s));
-                    tma_load(to + 2 * A_BYTES + p * B_BYTES, &map_b, MN_MAJOR ? n0 : k0, MN_MAJOR ? k0 : n0, z + p, full(s));
+                    const uint32_t to_b = to + 2 * A_BYTES + p * B_BYTES;
+                    if (MN_MAJOR) {
+#pragma unroll
+                        for (int c = 0; c < TILE_N / 128; ++c) tma_load(to_b + c * BOX64_BYTES, &map_b, n0 + 64 * c, k0, z + p, full(s));
+                    } else {
+                        tma_load(to_b, &map_b, k0, n0, z + p, full(s));
+                    }
                 }
             }
             // Whatever still comes to this block's shared memory must come before it ends: the copies in flight, and the products'
@@ -463,9 +473,9 @@ orth_tiled_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             }
             if (MODE == POLYNOMIAL) {                       // A's tile, where the result is going to be put together
                 if (ok) {
-                    mbar_expect(old_here, 4 * PANEL);
+                    mbar_expect(old_here, 4 * PANELS * PANEL);
                     for (int p = 0; p < 2; ++p)
-                        for (int c = 0; c < 2; ++c) tma_load(at + (c * 2 + p) * PANEL, &map_old, (int)col0 + 64 * c, (int)row0, z + p, old_here);
+                        for (int c = 0; c < 2 * PANELS; ++c) tma_load(at + (c * 2 + p) * PANEL, &map_old, (int)col0 + 64 * c, (int)row0, z + p, old_here);
                     ok = mbar_wait(old_here, 0);
                 }
             }
@@ -488,7 +498,7 @@ orth_tiled_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
 #pragma unroll
                     for (int k = 0; k < TILE_K / 16; ++k) {
                         const uint64_t da = operand_k_major(pa + k * 32, TILE_K * 2);
-                        const uint64_t db = MN_MAJOR ? operand_mn_major(pb + k * 2048, B_BYTES) : operand_k_major(pb + k * 32, TILE_K * 2);
+                        const uint64_t db = MN_MAJOR ? operand_mn_major(pb + k * 2048, BOX64_BYTES) : operand_k_major(pb + k * 32, TILE_K * 2);
                         tc_product<2>(tmem + b * TILE_N, da, db, shape, term > 0 || k > 0);
                     }
                 }
@@ -551,16 +561,15 @@ orth_tiled_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 }
             }
         } else if (ok) {
-            char* hi_panel = base + group * 2 * PANEL;
-            char* lo_panel = hi_panel + PANEL;
+            char* const panels = base + group * (2 * PANELS) * PANEL;     // hi and lo of 64 columns each
 #pragma unroll
             for (int c = 0; c < OWN; c += 8) {
-                const uint32_t at = panel_at(own_row, c);
+                char* const hi_at = panels + (c / 64) * 2 * PANEL + panel_at(own_row, c % 64);
                 uint4 hi, lo;
                 float* v = acc + c;
                 if (MODE == POLYNOMIAL) {
-                    hi = *(const uint4*)(hi_panel + at);
-                    lo = *(const uint4*)(lo_panel + at);
+                    hi = *(const uint4*)hi_at;
+                    lo = *(const uint4*)(hi_at + PANEL);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const float2 old = join2(((const uint32_t*)&hi)[j], ((const uint32_t*)&lo)[j]);
@@ -573,37 +582,40 @@ orth_tiled_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                     for (int j = 0; j < 8; ++j) v[j] *= MODE == GRAM ? FROM_XX * A_SCALE : FROM_BX * X_SCALE;
                 }
                 split8(v, hi, lo);
-                *(uint4*)(hi_panel + at) = hi;
-                *(uint4*)(lo_panel + at) = lo;
+                *(uint4*)hi_at = hi;
+                *(uint4*)(hi_at + PANEL) = lo;
             }
             const bool first = (threadIdx.x & 127) == 64;   // warps 2 to 5 and 6 to 9: one thread of each group
             const int z = 2 * (int)blockIdx.y;
             async_proxy_fence();
             group_sync(group);
-            if (first && row0 < t.m && col < t.n) {
-                tma_store(&map_to, (int)col, (int)row0, z, smem_address(hi_panel));
-                tma_store(&map_to, (int)col, (int)row0, z + 1, smem_address(lo_panel));
-                tma_store_commit();
-            }
-            if (SYMMETRIC && bj < 2 * bi) {                 // the tile's mirror image: 64 rows of 128 values, two panels of 64
+            if (first)
+                for (int q = 0; q < PANELS; ++q)
+                    if (row0 < t.m && col + 64 * q < t.n) {
+                        tma_store(&map_to, (int)col + 64 * q, (int)row0, z, smem_address(panels + 2 * q * PANEL));
+                        tma_store(&map_to, (int)col + 64 * q, (int)row0, z + 1, smem_address(panels + (2 * q + 1) * PANEL));
+                    }
+            if (first) tma_store_commit();
+            if (SYMMETRIC && col0 < bi * PAIR_M) {          // the mirror image: per 64 columns 64 rows of 128 values, two panels of 64
                 if (first) tma_store_wait_read();
                 group_sync(group);
 #pragma unroll
                 for (int j = 0; j < OWN; ++j) {
                     __half hi, lo;
                     split(acc[j], hi, lo);
-                    const uint32_t at = (own_row >> 6) * (PANEL / 2) + j * 128 + ((((own_row & 63) >> 3) ^ (j & 7)) << 4) + (own_row & 7) * 2;
-                    *(__half*)(hi_panel + at) = hi;
-                    *(__half*)(lo_panel + at) = lo;
+                    char* const at = panels + (j / 64) * 2 * PANEL + (own_row >> 6) * (PANEL / 2) + (j & 63) * 128 + ((((own_row & 63) >> 3) ^ (j & 7)) << 4) + (own_row & 7) * 2;
+                    *(__half*)at = hi;
+                    *(__half*)(at + PANEL) = lo;
                 }
                 async_proxy_fence();
                 group_sync(group);
                 if (first)
-                    for (int p = 0; p < 2; ++p)
-                        if (row0 + 64 * p < t.m) {
-                            tma_store(&map_mirror, (int)row0 + 64 * p, (int)col, z, smem_address(hi_panel + p * (PANEL / 2)));
-                            tma_store(&map_mirror, (int)row0 + 64 * p, (int)col, z + 1, smem_address(lo_panel + p * (PANEL / 2)));
-                        }
+                    for (int q = 0; q < PANELS; ++q)
+                        for (int p = 0; p < 2; ++p)
+                            if (row0 + 64 * p < t.m) {
+                                tma_store(&map_mirror, (int)row0 + 64 * p, (int)col + 64 * q, z, smem_address(panels + 2 * q * PANEL + p * (PANEL / 2)));
+                                tma_store(&map_mirror, (int)row0 + 64 * p, (int)col + 64 * q, z + 1, smem_address(panels + (2 * q + 1) * PANEL + p * (PANEL / 2)));
+                            }
                 if (first) tma_store_commit();
             }
             if (first) tma_store_wait();
@@ -695,14 +707,26 @@ uint64_t align_up(uint64_t x) { return (x + 255) / 256 * 256; }
 
 bool small_form(uint32_t m, uint32_t n) { return m <= SMALL_M && n <= SMALL_N; }
 
+uint64_t tile_pairs(uint32_t m, uint32_t n, bool symmetric, uint32_t tile_n)
+{
+    const uint32_t rows = (m + PAIR_M - 1) / PAIR_M;
+    uint64_t tiles = 0;
+    if (symmetric) for (uint32_t bi = 0; bi < rows; ++bi) tiles += tiles_of_rows(bi, tile_n);
+    else tiles = (uint64_t)rows * ((n + tile_n - 1) / tile_n);
+    return tiles;
+}
+// 256 or 128 columns per tile: what takes fewer rounds of the multiprocessors, a round of the narrower tiles counting half.
+uint32_t pick_tile(const nups_store* s, uint32_t batch, uint32_t m, uint32_t n, bool symmetric)
+{
+    const uint64_t pairs = (uint64_t)s->sm_count / 2;
+    const uint64_t wide = (tile_pairs(m, n, symmetric, 256) * batch + pairs - 1) / pairs, narrow = (tile_pairs(m, n, symmetric, 128) * batch + pairs - 1) / pairs;
+    return narrow < 2 * wide ? 128 : 256;
+}
 // Into how many pieces K of the Gram matrix is cut where its tiles alone would leave multiprocessors idle: pieces of at least
-// 512 values, two blocks per multiprocessor at most.
+// 512 values, one block per multiprocessor at most.
 uint32_t gram_slices(const nups_store* s, uint32_t batch, uint32_t m, uint32_t n)
 {
-    uint64_t blocks = 0;
-    for (uint32_t bi = 0; bi < (m + PAIR_M - 1) / PAIR_M; ++bi) blocks += 2 * (uint64_t)tiles_of_rows(bi);
-    blocks *= batch;
-    const uint64_t fit = 2 * (uint64_t)s->sm_count / blocks, pieces = n / 512;
+    const uint64_t fit = (uint64_t)s->sm_count / 2 / (tile_pairs(m, m, true, 128) * batch), pieces = n / 512;
     const uint64_t slices = fit < pieces ? fit : pieces;
     return slices < 2 ? 1 : slices > 8 ? 8 : (uint32_t)slices;
 }
@@ -729,26 +753,41 @@ nups_status buffer_maps(Maps* to, __half* p, uint32_t rows, uint32_t cols, uint3
     return plane_map(&to->rows64, p, rows, cols, ld, 2 * batch, 64, 64);
 }
 
-template <int MODE>
-nups_status launch_tiled(nups_store* s, const Maps& a, const Maps& b, const Maps& old, const Maps& to, const TiledArgs& t, const OrthArgs& o, unsigned tiles,
-                         unsigned batch, cudaStream_t st)
+template <int MODE, int TILE_N>
+nups_status launch_tiles(nups_store* s, const Maps& a, const Maps& b, const Maps& old, const Maps& to, const TiledArgs& t, const OrthArgs& o, unsigned batch, cudaStream_t st)
 {
-    CK(nups_launch_dependent(orth_tiled_kernel<MODE>, dim3(2 * tiles, batch, t.slices), TILED_BLOCK, TILED_SMEM, st, a.rows128, b.rows64, old.rows128, to.rows128, to.rows64,
-                             t, o));
+    constexpr bool SYMMETRIC = MODE == GRAM || MODE == POLYNOMIAL || MODE == PART;
+    const unsigned tiles = (unsigned)tile_pairs(t.m, t.n, SYMMETRIC, TILE_N);
+    TiledArgs u = t;
+    u.tiles_n = (t.n + TILE_N - 1) / TILE_N;
+    CK(nups_launch_dependent(orth_tiled_kernel<MODE, TILE_N>, dim3(2 * tiles, batch, t.slices), TILED_BLOCK, TILED_SMEM, st, a.rows128,
+                             SYMMETRIC && TILE_N == 256 ? b.rows128 : b.rows64, old.rows128, to.rows128, to.rows64, u, o));
     LAUNCH_CHECK(s);
     return NUPS_OK;
 }
+template <int MODE>
+nups_status launch_tiled(nups_store* s, const Maps& a, const Maps& b, const Maps& old, const Maps& to, const TiledArgs& t, const OrthArgs& o, unsigned batch, cudaStream_t st)
+{
+    constexpr bool SYMMETRIC = MODE == GRAM || MODE == POLYNOMIAL || MODE == PART;
+    if (MODE == PART || pick_tile(s, batch, t.m, t.n, SYMMETRIC) == 128) return launch_tiles<MODE, 128>(s, a, b, old, to, t, o, batch, st);
+    if constexpr (MODE != PART) return launch_tiles<MODE, 256>(s, a, b, old, to, t, o, batch, st);
+}
 
 // Large dynamic shared memory, asked for once on the store's device.
+template <int MODE, int TILE_N> cudaError_t opt_in_tiled() { return cudaFuncSetAttribute(orth_tiled_kernel<MODE, TILE_N>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TILED_SMEM); }
 nups_status opt_in(nups_store* s)
 {
     if (s->orth_smem_opted) return NUPS_OK;
     CK(cudaFuncSetAttribute(orthogonalize_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)small_smem(SMALL_M, SMALL_N)));
-    CK(cudaFuncSetAttribute(orth_tiled_kernel<GRAM>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TILED_SMEM));
-    CK(cudaFuncSetAttribute(orth_tiled_kernel<POLYNOMIAL>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TILED_SMEM));
-    CK(cudaFuncSetAttribute(orth_tiled_kernel<PRODUCT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TILED_SMEM));
-    CK(cudaFuncSetAttribute(orth_tiled_kernel<LAST>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TILED_SMEM));
-    CK(cudaFuncSetAttribute(orth_tiled_kernel<PART>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TILED_SMEM));
+    CK((opt_in_tiled<GRAM, 128>()));
+    CK((opt_in_tiled<GRAM, 256>()));
+    CK((opt_in_tiled<POLYNOMIAL, 128>()));
+    CK((opt_in_tiled<POLYNOMIAL, 256>()));
+    CK((opt_in_tiled<PRODUCT, 128>()));
+    CK((opt_in_tiled<PRODUCT, 256>()));
+    CK((opt_in_tiled<LAST, 128>()));
+    CK((opt_in_tiled<LAST, 256>()));
+    CK((opt_in_tiled<PART, 128>()));
     s->orth_smem_opted = true;
     return NUPS_OK;
 }
@@ -765,24 +804,21 @@ nups_status launch_large(nups_store* s, const OrthArgs& o, uint32_t batch, char*
     LAUNCH_CHECK(s);
     nups_launch_dependent(orth_split_kernel, dim3((o.n + 31) / 32, (o.m + 31) / 32, batch), 256, 0, st, o, p);
     LAUNCH_CHECK(s);
-    const uint32_t tiles_m = (o.m + PAIR_M - 1) / PAIR_M, tiles_n = (o.n + TILE_N - 1) / TILE_N;
-    uint32_t half = 0;
-    for (uint32_t bi = 0; bi < tiles_m; ++bi) half += tiles_of_rows(bi);
     const TiledArgs gram = {o.m, o.m, (o.n + TILE_K - 1) / TILE_K, 0, p.slices, p.part, p.lda};
     const TiledArgs polynomial = {o.m, o.m, (o.m + TILE_K - 1) / TILE_K, 0, 1, nullptr, p.lda};
-    const TiledArgs product = {o.m, o.n, (o.m + TILE_K - 1) / TILE_K, tiles_n, 1, nullptr, p.ldx};
+    const TiledArgs product = {o.m, o.n, (o.m + TILE_K - 1) / TILE_K, 0, 1, nullptr, p.ldx};
     for (uint32_t step = 0; step < o.steps; ++step) {
         const Maps &from = x[step & 1], &to = x[1 - (step & 1)];
         if (p.slices > 1) {
-            OK_OR_RETURN(launch_tiled<PART>(s, from, from, a, a, gram, o, half, batch, st));
+            OK_OR_RETURN(launch_tiled<PART>(s, from, from, a, a, gram, o, batch, st));
             nups_launch_dependent(orth_join_kernel, dim3((o.m + 63) / 64, (o.m + 63) / 64, batch), 256, 0, st, (const float*)p.part, p.slices, o.m, p.lda, p.a);
             LAUNCH_CHECK(s);
         } else {
-            OK_OR_RETURN(launch_tiled<GRAM>(s, from, from, a, a, gram, o, half, batch, st));
+            OK_OR_RETURN(launch_tiled<GRAM>(s, from, from, a, a, gram, o, batch, st));
         }
-        OK_OR_RETURN(launch_tiled<POLYNOMIAL>(s, a, a, a, b, polynomial, o, half, batch, st));
-        if (step + 1 < o.steps) OK_OR_RETURN(launch_tiled<PRODUCT>(s, b, from, a, to, product, o, tiles_m * tiles_n, batch, st));
-        else OK_OR_RETURN(launch_tiled<LAST>(s, b, from, a, to, product, o, tiles_m * tiles_n, batch, st));
+        OK_OR_RETURN(launch_tiled<POLYNOMIAL>(s, a, a, a, b, polynomial, o, batch, st));
+        if (step + 1 < o.steps) OK_OR_RETURN(launch_tiled<PRODUCT>(s, b, from, a, to, product, o, batch, st));
+        else OK_OR_RETURN(launch_tiled<LAST>(s, b, from, a, to, product, o, batch, st));
     }
     return NUPS_OK;
 }
