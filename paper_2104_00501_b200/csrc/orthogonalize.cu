@@ -342,7 +342,7 @@ __global__ void __launch_bounds__(256) orth_split_kernel(OrthArgs a, Planes p)
 }
 
 enum { GRAM = 0, POLYNOMIAL = 1, PRODUCT = 2, LAST = 3, PART = 4 };
-constexpr int BLOCK_M = 128, PAIR_M = 256, TILE_K = 64, TILED_BLOCK = 320, SUM_WARPS = 8;
+constexpr int BLOCK_M = 128, PAIR_M = 256, TILE_K = 64, SUM_WARPS = 16, TILED_BLOCK = 64 + 32 * SUM_WARPS;
 constexpr uint32_t A_BYTES = BLOCK_M * TILE_K * 2, BOX64_BYTES = 64 * TILE_K * 2;
 // One block per multiprocessor, and nothing beside it: two pairs that ask for tensor memory on the same two multiprocessors at
 // the same time could each hold the right to allocate on one of them and wait for it on the other.
@@ -356,14 +356,14 @@ struct TiledArgs {
     uint32_t ld;
 };
 
-// Barrier of the four warps that share 64 columns of a tile.
-__device__ __forceinline__ void group_sync(uint32_t group) { asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory"); }
-
+// Barrier of the THREADS threads that put 64 columns of a tile together.
+template <int THREADS> __device__ __forceinline__ void group_sync(uint32_t group) { asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(THREADS) : "memory"); }
 // ... and whether `ok` holds for all of them.
-__device__ __forceinline__ bool group_all(uint32_t group, bool ok)
+template <int THREADS> __device__ __forceinline__ bool group_all(uint32_t group, bool ok)
 {
     uint32_t r;
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbar.red.and.pred q, %2, 128, p;\n\tselp.b32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"((uint32_t)ok), "r"(1 + group) : "memory");
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbar.red.and.pred q, %2, %3, p;\n\tselp.b32 %0, 1, 0, q;\n\t}"
+                 : "=r"(r) : "r"((uint32_t)ok), "r"(1 + group), "n"(THREADS) : "memory");
     return r != 0;
 }
 
@@ -385,10 +385,10 @@ __device__ __forceinline__ void write_rows(void* out, int type, uint64_t at, uin
 
 // A tile of 256 x TILE_N results (128 or 256) by a pair of blocks, 128 rows each.  In each block warp 0 brings in the operands' pairs by TMA; warp 1
 // of the first block issues the products of both (cta_group::2: each block reads its own rows of A and half of B, so shared
-// memory is read and filled at two thirds of the rate that a block on its own would need); eight warps sum.  The tensor cores cut
+// memory is read and filled at two thirds of the rate that a block on its own would need); sixteen warps sum.  The tensor cores cut
 // what an addition shifts out, so a long sum in tensor memory drifts towards zero (1e-6 of a 1024-term sum, which the iteration
-// multiplies: 1e-4 of the result at 4096 x 4096).  Each run of TILE_K values of K therefore starts anew in one of two sets of
-// accumulators, the small products hi lo and lo hi first, and is added in registers, with rounding, while the next run is
+// multiplies: 1e-4 of the result at 4096 x 4096).  Each run of TILE_K values of K therefore starts anew in one of two or four sets
+// of accumulators, the small products hi lo and lo hi first, and is added in registers, with rounding, while the next run is
 // multiplied.
 // The result leaves through shared memory in the operands' layout, by TMA; below the diagonal a second, transposed time.
 template <int MODE, int TILE_N>
@@ -397,11 +397,13 @@ orth_tiled_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                   const __grid_constant__ CUtensorMap map_to, const __grid_constant__ CUtensorMap map_mirror, TiledArgs t, OrthArgs o)
 {
     constexpr bool SYMMETRIC = MODE == GRAM || MODE == POLYNOMIAL || MODE == PART, MN_MAJOR = !SYMMETRIC;
-    constexpr int OWN = TILE_N / 2, PANELS = OWN / 64;      // columns that a summing warp takes
+    constexpr int SETS = 512 / TILE_N;                      // of accumulators
+    constexpr int OWN = TILE_N / 4, PANELS = TILE_N / 64;   // columns that a summing warp takes; runs of 64 columns
+    constexpr int SHARERS = 32 * SUM_WARPS / PANELS;        // threads that put such a run together
     constexpr uint32_t B_BYTES = TILE_N / 2 * TILE_K * 2, STAGE_BYTES = 2 * (A_BYTES + B_BYTES), STAGES = TILE_N == 256 ? 3 : 4;
-    static_assert(STAGES * STAGE_BYTES + 1024 == TILED_SMEM && 4 * PANELS * PANEL <= STAGES * STAGE_BYTES, "shared memory of a block");
+    static_assert(STAGES * STAGE_BYTES + 1024 == TILED_SMEM && 2 * PANELS * PANEL <= STAGES * STAGE_BYTES, "shared memory of a block");
     extern __shared__ char raw[];
-    __shared__ uint64_t bars[3 * STAGES + 5];
+    __shared__ uint64_t bars[3 * STAGES + 2 * SETS + 1];
     __shared__ uint32_t tmem_mem;
     char* base = (char*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -423,16 +425,16 @@ orth_tiled_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     auto other = [&](uint32_t s) { return smem_address(&bars[STAGES + s]); };            // first block: the second's have
     auto empty = [&](uint32_t s) { return smem_address(&bars[2 * STAGES + s]); };
     auto summed = [&](uint32_t b) { return smem_address(&bars[3 * STAGES + b]); };       // first block: a set of accumulators is free
-    auto ready = [&](uint32_t b) { return smem_address(&bars[3 * STAGES + 2 + b]); };    // ... is complete
-    const uint32_t old_here = smem_address(&bars[3 * STAGES + 4]);
+    auto ready = [&](uint32_t b) { return smem_address(&bars[3 * STAGES + SETS + b]); };    // ... is complete
+    const uint32_t old_here = smem_address(&bars[3 * STAGES + 2 * SETS]);
     if (threadIdx.x == 0) {
         for (uint32_t s = 0; s < STAGES; ++s) { mbar_init(full(s), 1); mbar_init(other(s), 1); mbar_init(empty(s), 1); }
-        for (int b = 0; b < 2; ++b) { mbar_init(summed(b), 2 * SUM_WARPS); mbar_init(ready(b), 1); }
+        for (int b = 0; b < SETS; ++b) { mbar_init(summed(b), 2 * SUM_WARPS); mbar_init(ready(b), 1); }
         mbar_init(old_here, 1);
         mbar_init_visible();
     }
     __syncwarp();
-    if (warp == 1) tmem_alloc<2>(smem_address(&tmem_mem), 2 * TILE_N);
+    if (warp == 1) tmem_alloc<2>(smem_address(&tmem_mem), SETS * TILE_N);
     tc_fence_before();
     __syncthreads();
     cluster_arrive();
@@ -473,9 +475,9 @@ orth_tiled_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             }
             if (MODE == POLYNOMIAL) {                       // A's tile, where the result is going to be put together
                 if (ok) {
-                    mbar_expect(old_here, 4 * PANELS * PANEL);
+                    mbar_expect(old_here, 2 * PANELS * PANEL);
                     for (int p = 0; p < 2; ++p)
-                        for (int c = 0; c < 2 * PANELS; ++c) tma_load(at + (c * 2 + p) * PANEL, &map_old, (int)col0 + 64 * c, (int)row0, z + p, old_here);
+                        for (int c = 0; c < PANELS; ++c) tma_load(at + (c * 2 + p) * PANEL, &map_old, (int)col0 + 64 * c, (int)row0, z + p, old_here);
                     ok = mbar_wait(old_here, 0);
                 }
             }
@@ -485,8 +487,8 @@ orth_tiled_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             const uint32_t at = smem_address(base);
             constexpr uint32_t shape = product_shape<2>(TILE_N, MN_MAJOR);
             for (uint32_t kb = 0; kb < kbs; ++kb) {
-                const uint32_t s = kb % STAGES, b = kb & 1;
-                if ((kb >= 2 && !mbar_wait(summed(b), (kb / 2 - 1) & 1)) || !mbar_wait(full(s), (kb / STAGES) & 1) || !mbar_wait(other(s), (kb / STAGES) & 1)) {
+                const uint32_t s = kb % STAGES, b = kb % SETS;
+                if ((kb >= SETS && !mbar_wait(summed(b), (kb / SETS - 1) & 1)) || !mbar_wait(full(s), (kb / STAGES) & 1) || !mbar_wait(other(s), (kb / STAGES) & 1)) {
                     ok = false;
                     break;
                 }
@@ -513,30 +515,30 @@ orth_tiled_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             }
         }
     } else {
-        const uint32_t group = (warp - 2) / 4, quarter = (warp & 3) * 32, own_row = quarter + lane;
+        // four warps, one for each quarter of the rows, take OWN columns; group: the run of 64 columns that these belong to
+        const uint32_t own_col = (warp - 2) / 4 * OWN, group = own_col / 64, quarter = (warp & 3) * 32, own_row = quarter + lane;
         float acc[OWN];
 #pragma unroll
         for (int j = 0; j < OWN; ++j) acc[j] = 0.0f;
         for (uint32_t kb = 0; kb < kbs; ++kb) {
-            const uint32_t b = kb & 1;
-            ok = __all_sync(0xFFFFFFFFu, mbar_wait(ready(b), (kb / 2) & 1));
+            const uint32_t b = kb % SETS;
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait(ready(b), (kb / SETS) & 1));
             if (!ok) break;
             tc_fence_after();
 #pragma unroll
-            for (int c = 0; c < OWN; c += 16) {
-                float v[16];
-                tmem_load16(tmem + (quarter << 16) + b * TILE_N + group * OWN + c, v);
-                tmem_load_wait();
+            for (int c = 0; c < OWN; c += 32) {
+                float v[32];
+                tmem_load32(tmem + (quarter << 16) + b * TILE_N + own_col + c, v);
 #pragma unroll
-                for (int j = 0; j < 16; ++j) acc[c + j] += v[j];
+                for (int j = 0; j < 32; ++j) acc[c + j] += v[j];
             }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(smem_of_rank(summed(b), 0));
         }
         if (MODE == POLYNOMIAL) ok = ok && mbar_wait(old_here, 0);
-        ok = group_all(group, ok);
-        const uint32_t col = col0 + group * OWN;
+        ok = group_all<SHARERS>(group, ok);
+        const uint32_t col = col0 + own_col;
         if (MODE == LAST || MODE == PART) {
             float* tile = (float*)base + (warp - 2) * 32 * 33;
             const float f = MODE == PART ? FROM_XX * A_SCALE : FROM_BX * o.scale;
@@ -561,10 +563,11 @@ orth_tiled_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 }
             }
         } else if (ok) {
-            char* const panels = base + group * (2 * PANELS) * PANEL;     // hi and lo of 64 columns each
+            char* const panel = base + group * 2 * PANEL;   // hi, then lo, of the 64 columns
+            const uint32_t in_panel = own_col % 64, panel_col = col0 + group * 64;
 #pragma unroll
             for (int c = 0; c < OWN; c += 8) {
-                char* const hi_at = panels + (c / 64) * 2 * PANEL + panel_at(own_row, c % 64);
+                char* const hi_at = panel + panel_at(own_row, in_panel + c);
                 uint4 hi, lo;
                 float* v = acc + c;
                 if (MODE == POLYNOMIAL) {
@@ -585,38 +588,37 @@ orth_tiled_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 *(uint4*)hi_at = hi;
                 *(uint4*)(hi_at + PANEL) = lo;
             }
-            const bool first = (threadIdx.x & 127) == 64;   // warps 2 to 5 and 6 to 9: one thread of each group
+            const bool first = (threadIdx.x - 64) % SHARERS == 0;
             const int z = 2 * (int)blockIdx.y;
             async_proxy_fence();
-            group_sync(group);
-            if (first)
-                for (int q = 0; q < PANELS; ++q)
-                    if (row0 < t.m && col + 64 * q < t.n) {
-                        tma_store(&map_to, (int)col + 64 * q, (int)row0, z, smem_address(panels + 2 * q * PANEL));
-                        tma_store(&map_to, (int)col + 64 * q, (int)row0, z + 1, smem_address(panels + (2 * q + 1) * PANEL));
-                    }
-            if (first) tma_store_commit();
-            if (SYMMETRIC && col0 < bi * PAIR_M) {          // the mirror image: per 64 columns 64 rows of 128 values, two panels of 64
+            group_sync<SHARERS>(group);
+            if (first && row0 < t.m && panel_col < t.n) {
+                tma_store(&map_to, (int)panel_col, (int)row0, z, smem_address(panel));
+                tma_store(&map_to, (int)panel_col, (int)row0, z + 1, smem_address(panel + PANEL));
+                tma_store_commit();
+            }
+            if (SYMMETRIC && col0 < bi * PAIR_M) {          // the mirror image: 64 rows of 128 values, two panels of 64
                 if (first) tma_store_wait_read();
-                group_sync(group);
+                group_sync<SHARERS>(group);
 #pragma unroll
                 for (int j = 0; j < OWN; ++j) {
                     __half hi, lo;
                     split(acc[j], hi, lo);
-                    char* const at = panels + (j / 64) * 2 * PANEL + (own_row >> 6) * (PANEL / 2) + (j & 63) * 128 + ((((own_row & 63) >> 3) ^ (j & 7)) << 4) + (own_row & 7) * 2;
+                    const uint32_t r = in_panel + j;
+                    char* const at = panel + (own_row >> 6) * (PANEL / 2) + r * 128 + ((((own_row & 63) >> 3) ^ (r & 7)) << 4) + (own_row & 7) * 2;
                     *(__half*)at = hi;
                     *(__half*)(at + PANEL) = lo;
                 }
                 async_proxy_fence();
-                group_sync(group);
-                if (first)
-                    for (int q = 0; q < PANELS; ++q)
-                        for (int p = 0; p < 2; ++p)
-                            if (row0 + 64 * p < t.m) {
-                                tma_store(&map_mirror, (int)row0 + 64 * p, (int)col + 64 * q, z, smem_address(panels + 2 * q * PANEL + p * (PANEL / 2)));
-                                tma_store(&map_mirror, (int)row0 + 64 * p, (int)col + 64 * q, z + 1, smem_address(panels + (2 * q + 1) * PANEL + p * (PANEL / 2)));
-                            }
-                if (first) tma_store_commit();
+                group_sync<SHARERS>(group);
+                if (first) {
+                    for (int p = 0; p < 2; ++p)
+                        if (row0 + 64 * p < t.m) {
+                            tma_store(&map_mirror, (int)row0 + 64 * p, (int)panel_col, z, smem_address(panel + p * (PANEL / 2)));
+                            tma_store(&map_mirror, (int)row0 + 64 * p, (int)panel_col, z + 1, smem_address(panel + PANEL + p * (PANEL / 2)));
+                        }
+                    tma_store_commit();
+                }
             }
             if (first) tma_store_wait();
         }
@@ -628,7 +630,7 @@ orth_tiled_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     cluster_arrive();
     cluster_wait();                                         // nobody signals or reads the other block any more
     tc_fence_after();
-    if (warp == 1) tmem_free<2>(tmem, 2 * TILE_N);
+    if (warp == 1) tmem_free<2>(tmem, SETS * TILE_N);
 }
 
 // A from the slices' sums, 64 x 64 values per block of 256 threads; what lies below the diagonal blocks a second, transposed time.
