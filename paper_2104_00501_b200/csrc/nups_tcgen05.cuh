@@ -102,9 +102,9 @@ __device__ __forceinline__ uint64_t operand_mn_major(uint32_t address, uint32_t 
 }
 // Product of fp16 operands with fp32 accumulators, M = 128 P.  Of a pair each block holds its 128 rows of A and of the result, and
 // one half of B's N values.
-template <int P> __host__ __device__ constexpr uint32_t product_shape(int n, bool b_mn_major)
+template <int P> __host__ __device__ constexpr uint32_t product_shape(int n, bool b_mn_major, bool a_mn_major = false)
 {
-    return (1u << 4) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 * P >> 4) << 24);
+    return (1u << 4) | ((a_mn_major ? 1u : 0u) << 15) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 * P >> 4) << 24);
 }
 template <int P> __device__ __forceinline__ void tc_product(uint32_t d, uint64_t a, uint64_t b, uint32_t shape, bool add)
 {

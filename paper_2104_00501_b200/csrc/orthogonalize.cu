@@ -3,7 +3,7 @@
 // The iteration multiplies what it is given by up to a^steps where a singular value is small, so the roundings of 16-bit operands
 // would show: every number is held as a pair of fp16 values, hi + lo, 22 bits of it, and a product is hi hi + hi lo + lo hi with
 // fp32 accumulators.  Numbers are scaled by powers of two so that lo stays in the normal range: X by 2^14, A and the polynomial by
-// 2^13.  A and A^2 are symmetric: only tiles that reach the diagonal or lie below it are computed, and written twice.
+// 2^13.  A and A^2 are symmetric: only tiles that reach the diagonal or lie below it are computed.
 // The factor a goes onto the polynomial's diagonal, B = a I + b A + c A^2, so that the new X is one product, B X.
 //
 // Two forms.  Matrices of at most 128 x 256 (after transposing tall ones): one block per matrix holds X, A and B in shared memory
@@ -271,12 +271,19 @@ __global__ void __launch_bounds__(SMALL_BLOCK) orthogonalize_small_kernel(OrthAr
 // ---------------------------------------------------------------------------------------------
 namespace {
 
-constexpr int NORM_PARTS = 64;             // blocks that sum the squares of one matrix
+constexpr uint32_t NORM_RUN = 1024;        // values of a row that a block squares at a time
+// Blocks that sum the squares of one matrix.
+uint32_t norm_parts(uint32_t rows, uint32_t cols)
+{
+    const uint64_t runs = (uint64_t)rows * ((cols + NORM_RUN - 1) / NORM_RUN), parts = (runs + 7) / 8;
+    return parts > 512 ? 512 : (uint32_t)parts;
+}
 
 // Where the larger matrices' pairs lie: planes of fp16 values, hi then lo, per matrix; rows padded to 16 bytes.
 struct Planes {
     __half *x[2], *a, *b;
-    double* sums;              // [batch][NORM_PARTS]
+    double* sums;              // [batch][parts]
+    uint32_t parts;
     float* part;               // the Gram matrix's slices
     uint32_t ldx, lda, slices;
 };
@@ -286,55 +293,65 @@ __global__ void __launch_bounds__(256) orth_squares_kernel(OrthArgs a, double* s
     __shared__ double part[8];
     grid_dependency_wait();
     const char* g = (const char*)a.g + (uint64_t)blockIdx.y * a.gb * (a.type == NUPS_F32 ? 4 : 2);
+    const uint32_t per_row = (a.cols + NORM_RUN - 1) / NORM_RUN;
+    const uint64_t runs = (uint64_t)a.rows * per_row;
     double sum = 0;
-    for (uint32_t r = blockIdx.x; r < a.rows; r += NORM_PARTS)
-        for (uint32_t c = threadIdx.x; c < a.cols; c += 256 * 8) {
-            float x[8];
+    for (uint64_t run = blockIdx.x; run < runs; run += 4 * (uint64_t)gridDim.x) {
+        float x[16];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) x[k] = c + 256 * k < a.cols ? read_value(g, a.type, (uint64_t)r * a.gs + c + 256 * k) : 0.0f;
+        for (int u = 0; u < 4; ++u) {                       // four runs' loads in flight
+            const uint64_t i = run + u * (uint64_t)gridDim.x;
+            const uint32_t r = (uint32_t)(i / per_row), c = (uint32_t)(i % per_row) * NORM_RUN + threadIdx.x;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) sum += (double)x[k] * x[k];
+            for (int k = 0; k < 4; ++k) x[4 * u + k] = i < runs && c + 256 * k < a.cols ? read_value(g, a.type, (uint64_t)r * a.gs + c + 256 * k) : 0.0f;
         }
+#pragma unroll
+        for (int k = 0; k < 16; ++k) sum += (double)x[k] * x[k];
+    }
     sum = warp_sum_f64(sum);
     if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = sum;
     __syncthreads();
     if (threadIdx.x == 0) {
         sum = 0;
         for (int w = 0; w < 8; ++w) sum += part[w];
-        sums[blockIdx.y * NORM_PARTS + blockIdx.x] = sum;
+        sums[blockIdx.y * gridDim.x + blockIdx.x] = sum;
     }
 }
 
-// X's first pairs, 32 x 32 values per block of 32 x 8 threads; tall matrices are transposed through shared memory.
+// X's first pairs, 64 x 64 values per block of 256 threads; tall matrices are transposed through shared memory.
 __global__ void __launch_bounds__(256) orth_split_kernel(OrthArgs a, Planes p)
 {
-    __shared__ float tile[32][33];
-    __shared__ float factor;
+    __shared__ float tile[64][65];
+    __shared__ double part[8];
     grid_dependency_wait();
-    const uint32_t tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
-    if (ty == 0) {
-        double sum = 0;
-        for (int k = tx; k < NORM_PARTS; k += 32) sum += p.sums[blockIdx.z * NORM_PARTS + k];
-        sum = warp_sum_f64(sum);
-        if (tx == 0) factor = (float)((double)X_SCALE / (sqrt(sum) + (double)a.eps));
-    }
     const char* g = (const char*)a.g + (uint64_t)blockIdx.z * a.gb * (a.type == NUPS_F32 ? 4 : 2);
-    const uint32_t r0 = blockIdx.y * 32, c0 = blockIdx.x * 32;            // of X
-    for (uint32_t k = ty; k < 32; k += 8) {
-        const uint32_t gr = (a.tall ? c0 : r0) + k, gc = (a.tall ? r0 : c0) + tx;
-        const float x = gr < a.rows && gc < a.cols ? read_value(g, a.type, (uint64_t)gr * a.gs + gc) : 0.0f;
-        if (a.tall) tile[tx][k] = x;
-        else tile[k][tx] = x;
+    const uint32_t r0 = blockIdx.y * 64, c0 = blockIdx.x * 64, tx = threadIdx.x & 63, ty = threadIdx.x >> 6;      // of X
+    float v[16];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+        const uint32_t gr = (a.tall ? c0 : r0) + ty + 4 * k, gc = (a.tall ? r0 : c0) + tx;
+        v[k] = gr < a.rows && gc < a.cols ? read_value(g, a.type, (uint64_t)gr * a.gs + gc) : 0.0f;
     }
+    double sum = 0;
+    for (uint32_t k = threadIdx.x; k < p.parts; k += 256) sum += p.sums[blockIdx.z * p.parts + k];
+    sum = warp_sum_f64(sum);
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = sum;
+    if (a.tall)
+#pragma unroll
+        for (int k = 0; k < 16; ++k) tile[tx][ty + 4 * k] = v[k];
     __syncthreads();
-    const float f = factor;
+    sum = 0;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) sum += part[w];
+    const float f = (float)((double)X_SCALE / (sqrt(sum) + (double)a.eps));
     __half* hi = p.x[0] + (uint64_t)blockIdx.z * 2 * a.m * p.ldx;
     __half* lo = hi + (uint64_t)a.m * p.ldx;
-    for (uint32_t k = ty; k < 32; k += 8) {
-        const uint32_t r = r0 + k, c = c0 + tx;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+        const uint32_t r = r0 + ty + 4 * k, c = c0 + tx;
         if (r < a.m && c < a.n) {
             __half h, l;
-            split(tile[k][tx] * f, h, l);
+            split((a.tall ? tile[ty + 4 * k][tx] : v[k]) * f, h, l);
             hi[(uint64_t)r * p.ldx + c] = h;
             lo[(uint64_t)r * p.ldx + c] = l;
         }
@@ -390,13 +407,16 @@ __device__ __forceinline__ void write_rows(void* out, int type, uint64_t at, uin
 // multiplies: 1e-4 of the result at 4096 x 4096).  Each run of TILE_K values of K therefore starts anew in one of two or four sets
 // of accumulators, the small products hi lo and lo hi first, and is added in registers, with rounding, while the next run is
 // multiplied.
-// The result leaves through shared memory in the operands' layout, by TMA; below the diagonal a second, transposed time.
+// The result leaves through shared memory in the operands' layout, by TMA.  Of a symmetric matrix only the 256 x 256 blocks on and
+// below the diagonal are there; an operand's tile above it is its mirror image, brought in as it lies and read along the other
+// axis (MN-major).
 template <int MODE, int TILE_N>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TILED_BLOCK, 1)
-orth_tiled_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_old,
-                  const __grid_constant__ CUtensorMap map_to, const __grid_constant__ CUtensorMap map_mirror, TiledArgs t, OrthArgs o)
+orth_tiled_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_mirror,
+                  const __grid_constant__ CUtensorMap map_to, TiledArgs t, OrthArgs o)
 {
     constexpr bool SYMMETRIC = MODE == GRAM || MODE == POLYNOMIAL || MODE == PART, MN_MAJOR = !SYMMETRIC;
+    constexpr bool HALF_A = MODE == POLYNOMIAL || MODE == PRODUCT || MODE == LAST, HALF_B = MODE == POLYNOMIAL;   // operands of which only half is there
     constexpr int SETS = 512 / TILE_N;                      // of accumulators
     constexpr int OWN = TILE_N / 4, PANELS = TILE_N / 64;   // columns that a summing warp takes; runs of 64 columns
     constexpr int SHARERS = 32 * SUM_WARPS / PANELS;        // threads that put such a run together
@@ -426,6 +446,7 @@ orth_tiled_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     auto empty = [&](uint32_t s) { return smem_address(&bars[2 * STAGES + s]); };
     auto summed = [&](uint32_t b) { return smem_address(&bars[3 * STAGES + b]); };       // first block: a set of accumulators is free
     auto ready = [&](uint32_t b) { return smem_address(&bars[3 * STAGES + SETS + b]); };    // ... is complete
+    auto above = [&](int k0, uint32_t block) { return (uint32_t)k0 >= (block + 1) * PAIR_M; };   // columns from k0 of this block of 256 rows
     const uint32_t old_here = smem_address(&bars[3 * STAGES + 2 * SETS]);
     if (threadIdx.x == 0) {
         for (uint32_t s = 0; s < STAGES; ++s) { mbar_init(full(s), 1); mbar_init(other(s), 1); mbar_init(empty(s), 1); }
@@ -455,13 +476,19 @@ orth_tiled_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 const uint32_t to = at + s * STAGE_BYTES;
                 const int k0 = (int)((kb0 + kb) * TILE_K), n0 = (int)(col0 + rank * (TILE_N / 2));
                 mbar_expect(full(s), STAGE_BYTES);
+                const bool mirror_a = HALF_A && above(k0, bi), mirror_b = HALF_B && above(k0, col0 / PAIR_M);
 #pragma unroll
                 for (int p = 0; p < 2; ++p) {
-                    tma_load(to + p * A_BYTES, &map_a, k0, (int)row0, z + p, full(s));
-                    const uint32_t to_b = to + 2 * A_BYTES + p * B_BYTES;
-                    if (MN_MAJOR) {
+                    if (mirror_a) {
 #pragma unroll
-                        for (int c = 0; c < TILE_N / 128; ++c) tma_load(to_b + c * BOX64_BYTES, &map_b, n0 + 64 * c, k0, z + p, full(s));
+                        for (int c = 0; c < 2; ++c) tma_load(to + p * A_BYTES + c * BOX64_BYTES, &map_mirror, (int)row0 + 64 * c, k0, z + p, full(s));
+                    } else {
+                        tma_load(to + p * A_BYTES, &map_a, k0, (int)row0, z + p, full(s));
+                    }
+                    const uint32_t to_b = to + 2 * A_BYTES + p * B_BYTES;
+                    if (MN_MAJOR || mirror_b) {
+#pragma unroll
+                        for (int c = 0; c < TILE_N / 128; ++c) tma_load(to_b + c * BOX64_BYTES, MN_MAJOR ? &map_b : &map_mirror, n0 + 64 * c, k0, z + p, full(s));
                     } else {
                         tma_load(to_b, &map_b, k0, n0, z + p, full(s));
                     }
@@ -477,7 +504,7 @@ orth_tiled_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 if (ok) {
                     mbar_expect(old_here, 2 * PANELS * PANEL);
                     for (int p = 0; p < 2; ++p)
-                        for (int c = 0; c < PANELS; ++c) tma_load(at + (c * 2 + p) * PANEL, &map_old, (int)col0 + 64 * c, (int)row0, z + p, old_here);
+                        for (int c = 0; c < PANELS; ++c) tma_load(at + (c * 2 + p) * PANEL, &map_a, (int)col0 + 64 * c, (int)row0, z + p, old_here);
                     ok = mbar_wait(old_here, 0);
                 }
             }
@@ -485,7 +512,6 @@ orth_tiled_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     } else if (warp == 1) {
         if (lane == 0 && rank == 0) {
             const uint32_t at = smem_address(base);
-            constexpr uint32_t shape = product_shape<2>(TILE_N, MN_MAJOR);
             for (uint32_t kb = 0; kb < kbs; ++kb) {
                 const uint32_t s = kb % STAGES, b = kb % SETS;
                 if ((kb >= SETS && !mbar_wait(summed(b), (kb / SETS - 1) & 1)) || !mbar_wait(full(s), (kb / STAGES) & 1) || !mbar_wait(other(s), (kb / STAGES) & 1)) {
@@ -494,13 +520,16 @@ orth_tiled_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 }
                 tc_fence_after();
                 const uint32_t ah = at + s * STAGE_BYTES, bh = ah + 2 * A_BYTES;
+                const int k0 = (int)((kb0 + kb) * TILE_K);
+                const bool mn_a = HALF_A && above(k0, bi), mn_b = MN_MAJOR || (HALF_B && above(k0, col0 / PAIR_M));
+                const uint32_t shape = product_shape<2>(TILE_N, mn_b, mn_a);
 #pragma unroll
                 for (int term = 0; term < 3; ++term) {      // hi lo, lo hi, hi hi
                     const uint32_t pa = ah + (term == 1 ? A_BYTES : 0), pb = bh + (term == 0 ? B_BYTES : 0);
 #pragma unroll
                     for (int k = 0; k < TILE_K / 16; ++k) {
-                        const uint64_t da = operand_k_major(pa + k * 32, TILE_K * 2);
-                        const uint64_t db = MN_MAJOR ? operand_mn_major(pb + k * 2048, BOX64_BYTES) : operand_k_major(pb + k * 32, TILE_K * 2);
+                        const uint64_t da = mn_a ? operand_mn_major(pa + k * 2048, BOX64_BYTES) : operand_k_major(pa + k * 32, TILE_K * 2);
+                        const uint64_t db = mn_b ? operand_mn_major(pb + k * 2048, BOX64_BYTES) : operand_k_major(pb + k * 32, TILE_K * 2);
                         tc_product<2>(tmem + b * TILE_N, da, db, shape, term > 0 || k > 0);
                     }
                 }
@@ -597,29 +626,6 @@ orth_tiled_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 tma_store(&map_to, (int)panel_col, (int)row0, z + 1, smem_address(panel + PANEL));
                 tma_store_commit();
             }
-            if (SYMMETRIC && col0 < bi * PAIR_M) {          // the mirror image: 64 rows of 128 values, two panels of 64
-                if (first) tma_store_wait_read();
-                group_sync<SHARERS>(group);
-#pragma unroll
-                for (int j = 0; j < OWN; ++j) {
-                    __half hi, lo;
-                    split(acc[j], hi, lo);
-                    const uint32_t r = in_panel + j;
-                    char* const at = panel + (own_row >> 6) * (PANEL / 2) + r * 128 + ((((own_row & 63) >> 3) ^ (r & 7)) << 4) + (own_row & 7) * 2;
-                    *(__half*)at = hi;
-                    *(__half*)(at + PANEL) = lo;
-                }
-                async_proxy_fence();
-                group_sync<SHARERS>(group);
-                if (first) {
-                    for (int p = 0; p < 2; ++p)
-                        if (row0 + 64 * p < t.m) {
-                            tma_store(&map_mirror, (int)row0 + 64 * p, (int)panel_col, z, smem_address(panel + p * (PANEL / 2)));
-                            tma_store(&map_mirror, (int)row0 + 64 * p, (int)panel_col, z + 1, smem_address(panel + PANEL + p * (PANEL / 2)));
-                        }
-                    tma_store_commit();
-                }
-            }
             if (first) tma_store_wait();
         }
     }
@@ -633,47 +639,37 @@ orth_tiled_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     if (warp == 1) tmem_free<2>(tmem, SETS * TILE_N);
 }
 
-// A from the slices' sums, 64 x 64 values per block of 256 threads; what lies below the diagonal blocks a second, transposed time.
+// A from the slices' sums, 64 x 64 values per block of 256 threads, four at a time (ld is a multiple of 8).
 __global__ void __launch_bounds__(256) orth_join_kernel(const float* part, uint32_t slices, uint32_t m, uint32_t ld, __half* a)
 {
     const uint32_t c0 = blockIdx.x * 64, r0 = blockIdx.y * 64, batch = gridDim.z;
     if (c0 >= (r0 / PAIR_M + 1) * PAIR_M) return;           // not computed
-    __shared__ float tile[64][65];
     grid_dependency_wait();
-    const uint32_t tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
-    __half* hi = a + (uint64_t)blockIdx.z * 2 * m * ld;
-    __half* lo = hi + (uint64_t)m * ld;
-    float v[16];
+    const uint32_t c = c0 + (threadIdx.x & 15) * 4, ty = threadIdx.x >> 4;
+    if (c >= m) return;
+    float4 v[4];
 #pragma unroll
-    for (int k = 0; k < 16; ++k) v[k] = 0.0f;
+    for (int k = 0; k < 4; ++k) v[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 2
     for (uint32_t s = 0; s < slices; ++s) {
-        const float* from = part + ((uint64_t)s * batch + blockIdx.z) * m * ld + c0 + tx;
+        const float* from = part + ((uint64_t)s * batch + blockIdx.z) * m * ld + c;
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
-            const uint32_t r = r0 + ty + 4 * k;
-            if (r < m && c0 + tx < m) v[k] += __ldcg(from + (uint64_t)r * ld);
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t r = r0 + ty + 16 * k;
+            if (r < m) v[k] = add4(v[k], __ldcg((const float4*)(from + (uint64_t)r * ld)));
         }
     }
+    __half* hi = a + (uint64_t)blockIdx.z * 2 * m * ld + c;
+    __half* lo = hi + (uint64_t)m * ld;
 #pragma unroll
-    for (int k = 0; k < 16; ++k) {
-        const uint32_t r = r0 + ty + 4 * k, c = c0 + tx;
-        tile[ty + 4 * k][tx] = v[k];
-        if (r < m && c < m) {
-            __half h, l;
-            split(v[k], h, l);
-            hi[(uint64_t)r * ld + c] = h;
-            lo[(uint64_t)r * ld + c] = l;
-        }
-    }
-    if (c0 / PAIR_M == r0 / PAIR_M) return;                 // a diagonal block is computed in full
-    __syncthreads();
-    for (uint32_t k = ty; k < 64; k += 4) {
-        const uint32_t r = c0 + k, c = r0 + tx;
-        if (r < m && c < m) {
-            __half h, l;
-            split(tile[tx][k], h, l);
-            hi[(uint64_t)r * ld + c] = h;
-            lo[(uint64_t)r * ld + c] = l;
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t r = r0 + ty + 16 * k;
+        if (r < m) {                                        // values beyond m in a row's last run are not read by anybody
+            const __half2 h0 = __floats2half2_rn(v[k].x, v[k].y), h1 = __floats2half2_rn(v[k].z, v[k].w);
+            const float2 f0 = __half22float2(h0), f1 = __half22float2(h1);
+            const __half2 l0 = __floats2half2_rn(v[k].x - f0.x, v[k].y - f0.y), l1 = __floats2half2_rn(v[k].z - f1.x, v[k].w - f1.y);
+            *(uint2*)(hi + (uint64_t)r * ld) = make_uint2(*(const uint32_t*)&h0, *(const uint32_t*)&h1);
+            *(uint2*)(lo + (uint64_t)r * ld) = make_uint2(*(const uint32_t*)&l0, *(const uint32_t*)&l1);
         }
     }
 }
@@ -717,27 +713,30 @@ uint64_t tile_pairs(uint32_t m, uint32_t n, bool symmetric, uint32_t tile_n)
     else tiles = (uint64_t)rows * ((n + tile_n - 1) / tile_n);
     return tiles;
 }
-// 256 or 128 columns per tile: what takes fewer rounds of the multiprocessors, a round of the narrower tiles counting half.
+// 256 or 128 columns per tile: what takes less time in rounds of the multiprocessors.  A run of K takes 1,550 cycles with 256
+// columns (the products' own time) and 1,270 with 128, where reading the operands bounds the products: a round of the narrower
+// tiles takes five sixths of the wider ones' time.
 uint32_t pick_tile(const nups_store* s, uint32_t batch, uint32_t m, uint32_t n, bool symmetric)
 {
     const uint64_t pairs = (uint64_t)s->sm_count / 2;
     const uint64_t wide = (tile_pairs(m, n, symmetric, 256) * batch + pairs - 1) / pairs, narrow = (tile_pairs(m, n, symmetric, 128) * batch + pairs - 1) / pairs;
-    return narrow < 2 * wide ? 128 : 256;
+    return 5 * narrow < 6 * wide ? 128 : 256;
 }
 // Into how many pieces K of the Gram matrix is cut where its tiles alone would leave multiprocessors idle: pieces of at least
 // 512 values, one block per multiprocessor at most.
 uint32_t gram_slices(const nups_store* s, uint32_t batch, uint32_t m, uint32_t n)
 {
-    const uint64_t fit = (uint64_t)s->sm_count / 2 / (tile_pairs(m, m, true, 128) * batch), pieces = n / 512;
+    const uint64_t fit = (uint64_t)s->sm_count / 2 / (tile_pairs(m, m, true, 256) * batch), pieces = n / 512;
     const uint64_t slices = fit < pieces ? fit : pieces;
     return slices < 2 ? 1 : slices > 8 ? 8 : (uint32_t)slices;
 }
 
-uint64_t planes_layout(const nups_store* s, uint32_t batch, uint32_t m, uint32_t n, char* base, Planes* p)
+uint64_t planes_layout(const nups_store* s, uint32_t batch, uint32_t rows, uint32_t cols, char* base, Planes* p)
 {
-    const uint32_t ldx = up(n, 8), lda = up(m, 8), slices = gram_slices(s, batch, m, n);
-    const uint64_t xb = align_up((uint64_t)batch * 2 * m * ldx * 2), ab = align_up((uint64_t)batch * 2 * m * lda * 2), sb = align_up((uint64_t)batch * NORM_PARTS * 8);
-    if (p) *p = {{(__half*)base, (__half*)(base + xb)}, (__half*)(base + 2 * xb), (__half*)(base + 2 * xb + ab), (double*)(base + 2 * xb + 2 * ab),
+    const uint32_t m = rows < cols ? rows : cols, n = rows < cols ? cols : rows;
+    const uint32_t ldx = up(n, 8), lda = up(m, 8), slices = gram_slices(s, batch, m, n), parts = norm_parts(rows, cols);
+    const uint64_t xb = align_up((uint64_t)batch * 2 * m * ldx * 2), ab = align_up((uint64_t)batch * 2 * m * lda * 2), sb = align_up((uint64_t)batch * parts * 8);
+    if (p) *p = {{(__half*)base, (__half*)(base + xb)}, (__half*)(base + 2 * xb), (__half*)(base + 2 * xb + ab), (double*)(base + 2 * xb + 2 * ab), parts,
                  (float*)(base + 2 * xb + 2 * ab + sb), ldx, lda, slices};
     return 2 * xb + 2 * ab + sb + (slices > 1 ? (uint64_t)slices * batch * m * lda * 4 : 0);
 }
@@ -756,23 +755,24 @@ nups_status buffer_maps(Maps* to, __half* p, uint32_t rows, uint32_t cols, uint3
 }
 
 template <int MODE, int TILE_N>
-nups_status launch_tiles(nups_store* s, const Maps& a, const Maps& b, const Maps& old, const Maps& to, const TiledArgs& t, const OrthArgs& o, unsigned batch, cudaStream_t st)
+nups_status launch_tiles(nups_store* s, const Maps& a, const Maps& b, const Maps& to, const TiledArgs& t, const OrthArgs& o, unsigned batch, cudaStream_t st)
 {
     constexpr bool SYMMETRIC = MODE == GRAM || MODE == POLYNOMIAL || MODE == PART;
     const unsigned tiles = (unsigned)tile_pairs(t.m, t.n, SYMMETRIC, TILE_N);
     TiledArgs u = t;
     u.tiles_n = (t.n + TILE_N - 1) / TILE_N;
     CK(nups_launch_dependent(orth_tiled_kernel<MODE, TILE_N>, dim3(2 * tiles, batch, t.slices), TILED_BLOCK, TILED_SMEM, st, a.rows128,
-                             SYMMETRIC && TILE_N == 256 ? b.rows128 : b.rows64, old.rows128, to.rows128, to.rows64, u, o));
+                             SYMMETRIC && TILE_N == 256 ? b.rows128 : b.rows64, a.rows64, to.rows128, u, o));
     LAUNCH_CHECK(s);
     return NUPS_OK;
 }
 template <int MODE>
-nups_status launch_tiled(nups_store* s, const Maps& a, const Maps& b, const Maps& old, const Maps& to, const TiledArgs& t, const OrthArgs& o, unsigned batch, cudaStream_t st)
+nups_status launch_tiled(nups_store* s, const Maps& a, const Maps& b, const Maps& to, const TiledArgs& t, const OrthArgs& o, unsigned batch, cudaStream_t st)
 {
     constexpr bool SYMMETRIC = MODE == GRAM || MODE == POLYNOMIAL || MODE == PART;
-    if (MODE == PART || pick_tile(s, batch, t.m, t.n, SYMMETRIC) == 128) return launch_tiles<MODE, 128>(s, a, b, old, to, t, o, batch, st);
-    if constexpr (MODE != PART) return launch_tiles<MODE, 256>(s, a, b, old, to, t, o, batch, st);
+    if constexpr (MODE != PART)
+        if (pick_tile(s, batch, t.m, t.n, SYMMETRIC) == 128) return launch_tiles<MODE, 128>(s, a, b, to, t, o, batch, st);
+    return launch_tiles<MODE, 256>(s, a, b, to, t, o, batch, st);
 }
 
 // Large dynamic shared memory, asked for once on the store's device.
@@ -789,7 +789,7 @@ nups_status opt_in(nups_store* s)
     CK((opt_in_tiled<PRODUCT, 256>()));
     CK((opt_in_tiled<LAST, 128>()));
     CK((opt_in_tiled<LAST, 256>()));
-    CK((opt_in_tiled<PART, 128>()));
+    CK((opt_in_tiled<PART, 256>()));
     s->orth_smem_opted = true;
     return NUPS_OK;
 }
@@ -797,14 +797,14 @@ nups_status opt_in(nups_store* s)
 nups_status launch_large(nups_store* s, const OrthArgs& o, uint32_t batch, char* scratch, cudaStream_t st)
 {
     Planes p;
-    planes_layout(s, batch, o.m, o.n, scratch, &p);
+    planes_layout(s, batch, o.rows, o.cols, scratch, &p);
     Maps x[2], a, b;
     for (int i = 0; i < 2; ++i) OK_OR_RETURN(buffer_maps(&x[i], p.x[i], o.m, o.n, p.ldx, batch));
     OK_OR_RETURN(buffer_maps(&a, p.a, o.m, o.m, p.lda, batch));
     OK_OR_RETURN(buffer_maps(&b, p.b, o.m, o.m, p.lda, batch));
-    nups_launch_dependent(orth_squares_kernel, dim3(NORM_PARTS, batch), 256, 0, st, o, p.sums);
+    nups_launch_dependent(orth_squares_kernel, dim3(p.parts, batch), 256, 0, st, o, p.sums);
     LAUNCH_CHECK(s);
-    nups_launch_dependent(orth_split_kernel, dim3((o.n + 31) / 32, (o.m + 31) / 32, batch), 256, 0, st, o, p);
+    nups_launch_dependent(orth_split_kernel, dim3((o.n + 63) / 64, (o.m + 63) / 64, batch), 256, 0, st, o, p);
     LAUNCH_CHECK(s);
     const TiledArgs gram = {o.m, o.m, (o.n + TILE_K - 1) / TILE_K, 0, p.slices, p.part, p.lda};
     const TiledArgs polynomial = {o.m, o.m, (o.m + TILE_K - 1) / TILE_K, 0, 1, nullptr, p.lda};
@@ -812,15 +812,15 @@ nups_status launch_large(nups_store* s, const OrthArgs& o, uint32_t batch, char*
     for (uint32_t step = 0; step < o.steps; ++step) {
         const Maps &from = x[step & 1], &to = x[1 - (step & 1)];
         if (p.slices > 1) {
-            OK_OR_RETURN(launch_tiled<PART>(s, from, from, a, a, gram, o, batch, st));
+            OK_OR_RETURN(launch_tiled<PART>(s, from, from, a, gram, o, batch, st));
             nups_launch_dependent(orth_join_kernel, dim3((o.m + 63) / 64, (o.m + 63) / 64, batch), 256, 0, st, (const float*)p.part, p.slices, o.m, p.lda, p.a);
             LAUNCH_CHECK(s);
         } else {
-            OK_OR_RETURN(launch_tiled<GRAM>(s, from, from, a, a, gram, o, batch, st));
+            OK_OR_RETURN(launch_tiled<GRAM>(s, from, from, a, gram, o, batch, st));
         }
-        OK_OR_RETURN(launch_tiled<POLYNOMIAL>(s, a, a, a, b, polynomial, o, batch, st));
-        if (step + 1 < o.steps) OK_OR_RETURN(launch_tiled<PRODUCT>(s, b, from, a, to, product, o, batch, st));
-        else OK_OR_RETURN(launch_tiled<LAST>(s, b, from, a, to, product, o, batch, st));
+        OK_OR_RETURN(launch_tiled<POLYNOMIAL>(s, a, a, b, polynomial, o, batch, st));
+        if (step + 1 < o.steps) OK_OR_RETURN(launch_tiled<PRODUCT>(s, b, from, to, product, o, batch, st));
+        else OK_OR_RETURN(launch_tiled<LAST>(s, b, from, to, product, o, batch, st));
     }
     return NUPS_OK;
 }
@@ -854,7 +854,7 @@ extern "C" nups_status nups_orthogonalize_scratch(nups_store* s, uint32_t batch,
 {
     if (!s || !h_bytes_out || batch > 65535 || rows < 1 || cols < 1 || rows > NUPS_ORTHOGONALIZE_MAX_SIZE || cols > NUPS_ORTHOGONALIZE_MAX_SIZE) return NUPS_EINVAL;
     const uint32_t m = rows < cols ? rows : cols, n = rows < cols ? cols : rows;
-    *h_bytes_out = small_form(m, n) || batch == 0 ? 0 : planes_layout(s, batch, m, n, nullptr, nullptr);
+    *h_bytes_out = small_form(m, n) || batch == 0 ? 0 : planes_layout(s, batch, rows, cols, nullptr, nullptr);
     return NUPS_OK;
 }
 
