@@ -73,7 +73,8 @@ def check_forward(x, w, b, eps, y, mean, rstd):
 
 
 SHAPES = [(1, 1), (5, 2), (3, 3), (1, 64), (7, 64), (33, 100), (64, 101), (300, 128), (9, 129), (40, 300), (17, 511), (5, 513), (6, 1000),
-          (12, 1024), (3, 1500), (5, 2050), (2, 4096), (4, 4097), (2, 8192), (3, 8200), (1, 16384), (2, 20000), (2500, 32), (700, 500)]
+          (12, 1024), (3, 1500), (5, 2050), (2, 4096), (4, 4097), (2, 8192), (3, 8200), (1, 16384), (2, 20000), (2500, 32), (700, 500),
+          (301, 640), (601, 1024), (299, 2048), (303, 4096), (170, 8200), (151, 16384), (150, 33000)]
 
 
 @pytest.mark.parametrize("dtype", [F32, F64, F16, BF16])
