@@ -1,11 +1,14 @@
 // A router over experts: softmax and choice of the largest logits per item, counts per expert, balance and z losses, and the
 // gradient of the logits.
 //
-// One pass over the logits per direction.  An item's logits are held in the registers of a team of TPR lanes (EPT each).  The
-// choice takes one reduction over the team per chosen expert: each lane keeps its two largest logits as whole numbers in the
-// order of the logits (for 16-bit types with the expert's number in the bits that the logit leaves free, so that equal logits
-// are told apart by the same comparison), and looks through its logits again only when both were chosen.  The sums over items
-// (P, lse^2) stay in registers until the block ends; blocks leave them in scratch and a last small kernel adds them in order.
+// One pass over the logits per direction.  An item's logits are held in the registers of a team of TPR lanes (EPT each; few lanes
+// with many logits, so that what the team does together is shared by several items of a warp).  The choice takes one reduction over
+// the team per chosen expert: each lane keeps its KEPT largest logits as whole numbers in the order of the logits (for 16-bit types
+// with the expert's number in the bits that the logit leaves free, so that equal logits are told apart by the same comparison), and
+// looks through its logits again only when all of those were chosen.  The sums over items (P, lse^2) stay in registers until the
+// block ends; the four blocks of a cluster add theirs through shared memory and leave them in scratch, and a last small kernel
+// adds the clusters' in order.
+#include <atomic>
 #include <cooperative_groups.h>
 #include <math.h>
 #include <math_constants.h>
@@ -29,7 +32,7 @@ struct RouteArgs {
     uint32_t* part_c;          // [blocks][experts] counts, then [blocks] items
 };
 
-constexpr int ROUTE_BLOCK = 256;
+constexpr int ROUTE_BLOCK = 256, ROUTE_CLUSTER = 4;
 __host__ __device__ constexpr int route_slots(int tpr) { return tpr == 32 ? 1 : 4; }      // chosen experts that a lane keeps
 
 template <int TPR> __device__ __forceinline__ float lanes_sum(float x)
@@ -59,21 +62,66 @@ template <int TPR> __device__ __forceinline__ uint32_t lanes_min(uint32_t x)
     }
 }
 
-// Whole numbers in the order of the logits; 0 = never chosen (-infinity, NaN).  -0 counts as +0.
+// Whole numbers in the order of the logits; up to NONE = never chosen (-infinity).  -0 counts as +0; x is not NaN.
+constexpr uint32_t NONE = 0x007FFFFFu;
 __device__ __forceinline__ uint32_t ordered(float x)
 {
     const uint32_t b = __float_as_uint(x + 0.0f);
-    return x > -CUDART_INF_F ? b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u) : 0u;
+    return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float from_ordered(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u); }
 // fp16 and bf16 leave at least 13 bits of a float's mantissa free: the larger number there is the lower expert
 constexpr uint32_t FREE = 0x1FFFu;
-__device__ __forceinline__ uint32_t ordered_with(float x, uint32_t e)
-{
-    const uint32_t u = ordered(x);
-    return u ? (u & ~FREE) | (FREE - e) : 0u;
-}
+__device__ __forceinline__ uint32_t ordered_with(float x, uint32_t e) { return (ordered(x) & ~FREE) | (FREE - e); }
 __device__ __forceinline__ float logit_of(uint32_t key) { return from_ordered(key & 0x80000000u ? key & ~FREE : key | FREE); }
+
+// The largest keys of a lane, in order, each with its expert (PACKED: in the key).
+template <bool PACKED, int KEPT> struct Largest {
+    uint32_t key[KEPT], expert[PACKED ? 1 : KEPT];
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int i = 0; i < KEPT; ++i) key[i] = 0;
+    }
+    __device__ __forceinline__ void take(uint32_t k, uint32_t e)
+    {
+        if constexpr (PACKED) {
+#pragma unroll
+            for (int i = 0; i < KEPT; ++i) {
+                const uint32_t more = max(key[i], k);
+                k = min(key[i], k);
+                key[i] = more;
+            }
+        } else {                                            // experts come in ascending order: an equal key stays behind
+            bool more = false;
+#pragma unroll
+            for (int i = 0; i < KEPT; ++i) {
+                more = more || k > key[i];                  // what is behind its place moves down, equal or not
+                const uint32_t tk = more ? key[i] : k, te = more ? expert[i] : e;
+                key[i] = more ? k : key[i];
+                expert[i] = more ? e : expert[i];
+                k = tk;
+                e = te;
+            }
+        }
+    }
+    __device__ __forceinline__ void drop()
+    {
+#pragma unroll
+        for (int i = 0; i + 1 < KEPT; ++i) {
+            key[i] = key[i + 1];
+            if constexpr (!PACKED) expert[i] = expert[i + 1];
+        }
+        key[KEPT - 1] = 0;
+    }
+};
+
+__device__ __forceinline__ float exp2_fast(float x)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
 
 template <int TPR, int VEC> __device__ __forceinline__ uint32_t expert_at(int i, int t)
 {
@@ -111,15 +159,29 @@ __device__ __forceinline__ void finish_losses(const RouteArgs& a, float b, float
     a.loss[2] = Z;
 }
 
+// e^(x - most), elementwise
+template <int EPT> __device__ __forceinline__ void exponentials(const float (&x)[EPT], float most, float (&ex)[EPT])
+{
+    const float minus = -most, log2e = 1.4426950408889634f;
+    run_add<EPT, true>(ex, x, &minus);
+    run_scale<EPT>(ex, ex, log2e);
+#pragma unroll
+    for (int i = 0; i < EPT; ++i) ex[i] = exp2_fast(ex[i]);
+}
+
 template <class X, int VEC, int TPR, int EPT>
-__global__ void __launch_bounds__(ROUTE_BLOCK) route_kernel(RouteArgs a)
+__global__ void __launch_bounds__(ROUTE_BLOCK, EPT <= 8 ? 4 : EPT <= 16 ? 3 : 2) route_kernel(RouteArgs a)
 {
     constexpr int TEAMS = ROUTE_BLOCK / TPR, CAP = TPR * EPT, SLOTS = route_slots(TPR), WARPS = ROUTE_BLOCK / 32;
     constexpr bool PACKED = sizeof(X) == 2;
+    constexpr int KEPT = PACKED ? (EPT < 8 ? 2 : 4) : 2;
     __shared__ uint32_t chosen[CAP];                        // counts of this block
     __shared__ float sums[WARPS][CAP > 512 ? 512 : CAP];
-    __shared__ float zsum[WARPS];
+    __shared__ float psum[CAP];
+    __shared__ float zsum[WARPS], bsum[WARPS];
     __shared__ uint32_t tsum[WARPS];
+    __shared__ float z_block;
+    __shared__ uint32_t t_block;
     for (int e = threadIdx.x; e < CAP; e += ROUTE_BLOCK) chosen[e] = 0;
     __syncthreads();
     grid_dependency_wait();
@@ -132,84 +194,80 @@ __global__ void __launch_bounds__(ROUTE_BLOCK) route_kernel(RouteArgs a)
         const uint64_t row = base + team;
         const bool in = row < a.n;
         bool on = in && (!a.active || a.active[row]);
-        float x[EPT];
+        float x[EPT], ex[EPT], total, most;
         load_logits<X, VEC, TPR, EPT>((const X*)a.logits + row * a.stride, on, a.experts, t, -CUDART_INF_F, x);
-        // the lane's two largest
-        uint32_t first = 0, second = 0, e_first = 0;
-#pragma unroll
-        for (int i = 0; i < EPT; ++i) {
-            const uint32_t e = expert_at<TPR, VEC>(i, t);
-            const uint32_t u = PACKED ? ordered_with(x[i], e) : ordered(x[i]);
-            if (PACKED) second = max(second, min(first, u));
-            if (u > first) { first = u; e_first = e; }
-        }
         uint32_t slot_u[SLOTS];
         int32_t slot_e[SLOTS];
-        float most = 0;
-        bool any = false;
+        bool any, again = false;
+        auto key_of = [&](int i) { return PACKED ? ordered_with(x[i], expert_at<TPR, VEC>(i, t)) : ordered(x[i]); };
+        do {
+            Largest<PACKED, KEPT> top;
+            int left = 0;                                   // of those kept
+            uint32_t u = 0xFFFFFFFFu, e = 0;                // the last one chosen
+            most = 0.0f;
+            any = false;
 #pragma unroll
-        for (int s = 0; s < SLOTS; ++s) {
-            slot_u[s] = 0;
-            slot_e[s] = -1;
-            if (s * TPR >= (int)a.top) continue;
-            for (int l = 0; l < TPR; ++l) {
-                if (s * TPR + l >= (int)a.top) break;
-                const uint32_t u = lanes_max<TPR>(first);
-                uint32_t e;
-                if (PACKED) {
-                    e = FREE - (u & FREE);
-                    if (first == u) {
-                        first = second;
-                        second = 0;
-                        if (first == 0) {                   // both were chosen: look for the next two among all
-#pragma unroll
-                            for (int i = 0; i < EPT; ++i) {
-                                const uint32_t w = ordered_with(x[i], expert_at<TPR, VEC>(i, t));
-                                const uint32_t below = w < u ? w : 0u;
-                                second = max(second, min(first, below));
-                                first = max(first, below);
-                            }
-                        }
-                    }
-                } else {
-                    e = lanes_min<TPR>(first == u ? e_first : 0xFFFFFFFFu);
-                    if (first == u && e_first == e && u) {  // the lane's next: smaller, or equal and further on
-                        uint32_t next = 0, e_next = 0;
+            for (int s = 0; s < SLOTS; ++s) {
+                slot_u[s] = 0;
+                slot_e[s] = -1;
+                if (s * TPR >= (int)a.top) continue;
+                for (int l = 0; l < TPR; ++l) {
+                    if (s * TPR + l >= (int)a.top) break;
+                    if (left == 0) {                        // none are kept (any more): the largest after u
+                        left = KEPT;
+                        top.clear();
 #pragma unroll
                         for (int i = 0; i < EPT; ++i) {
-                            const uint32_t w = ordered(x[i]), ei = expert_at<TPR, VEC>(i, t);
-                            if ((w < u || (w == u && ei > e)) && w > next) { next = w; e_next = ei; }
+                            const uint32_t w = key_of(i), ei = expert_at<TPR, VEC>(i, t);
+                            top.take(w < u || (!PACKED && w == u && ei > e) ? w : 0u, ei);
                         }
-                        first = next;
-                        e_first = e_next;
                     }
+                    u = lanes_max<TPR>(top.key[0]);
+                    if constexpr (PACKED) e = FREE - (u & FREE);
+                    else e = lanes_min<TPR>(top.key[0] == u ? top.expert[0] : 0xFFFFFFFFu);
+                    bool mine = top.key[0] == u;
+                    if constexpr (!PACKED) mine = mine && top.expert[0] == e;
+                    if (mine) {
+                        top.drop();
+                        --left;
+                    }
+                    const bool some = u > (PACKED ? NONE | FREE : NONE);
+                    if (s == 0 && l == 0) {
+                        any = some;
+                        most = any ? (PACKED ? logit_of(u) : from_ordered(u)) : 0.0f;
+                    }
+                    if (t == l && some) { slot_u[s] = u; slot_e[s] = (int32_t)e; }
                 }
-                if (s == 0 && l == 0) {
-                    any = u != 0;
-                    most = any ? (PACKED ? logit_of(u) : from_ordered(u)) : 0.0f;
-                }
-                if (t == l && u) { slot_u[s] = u; slot_e[s] = (int32_t)e; }
             }
-        }
-        float ex[EPT], total = 0;
+            exponentials<EPT>(x, most, ex);
+            float two_sums[2] = {0, 0};
+            sum_run<EPT>(two_sums, ex);
+            total = lanes_sum<TPR>(two_sums[0] + two_sums[1]);
+            // NaN: the order above is void.  Once more without the NaN, which then are not chosen; the item's sum stays NaN.
+            if (again) total = CUDART_NAN_F;
+            again = !again && total != total;
+            bool nan_here = false;
 #pragma unroll
-        for (int i = 0; i < EPT; ++i) {
-            ex[i] = __expf(x[i] - most);
-            total += ex[i];
-        }
-        total = lanes_sum<TPR>(total);
+            for (int i = 0; i < EPT; ++i) {
+                nan_here = nan_here || x[i] != x[i];
+                if (again && x[i] != x[i]) x[i] = -CUDART_INF_F;
+            }
+            const bool nan_there = lanes_max<TPR>(nan_here ? 1u : 0u) != 0;       // by all lanes of the warp
+            again = again && nan_there;                     // +infinity does it too, and is in order
+        } while (__any_sync(0xFFFFFFFFu, again));
         if (!any && total == 0.0f) on = false;              // nothing but -infinity
         const float inv = on ? 1.0f / total : 0.0f;
         float kept[SLOTS], kept_sum = 0;
 #pragma unroll
         for (int s = 0; s < SLOTS; ++s) {
-            kept[s] = slot_e[s] >= 0 ? __expf((PACKED ? logit_of(slot_u[s]) : from_ordered(slot_u[s])) - most) : 0.0f;
+            kept[s] = slot_e[s] >= 0 ? exp2_fast(((PACKED ? logit_of(slot_u[s]) : from_ordered(slot_u[s])) - most) * 1.4426950408889634f) : 0.0f;
             kept_sum += kept[s];
         }
         float scale = inv;
         if (a.renormalize) {
             kept_sum = lanes_sum<TPR>(kept_sum);
             scale = kept_sum != 0.0f ? 1.0f / kept_sum : 0.0f;
+            if (total != total) scale = total;
         }
         if (in) {
 #pragma unroll
@@ -229,9 +287,7 @@ __global__ void __launch_bounds__(ROUTE_BLOCK) route_kernel(RouteArgs a)
                 zacc += lse * lse;
                 ++items;
             }
-            if (a.sums)
-#pragma unroll
-                for (int i = 0; i < EPT; ++i) acc[i] += ex[i] * inv;
+            if (a.sums) run_fma<EPT, false, true, false>(acc, ex, &inv, acc);
         } else if (in && t == 0 && a.lse) {
             a.lse[row] = 0.0f;
         }
@@ -250,10 +306,7 @@ __global__ void __launch_bounds__(ROUTE_BLOCK) route_kernel(RouteArgs a)
     uint32_t m = 0;
 #pragma unroll
     for (int w = 0; w < WARPS; ++w) { z += zsum[w]; m += tsum[w]; }
-    const bool alone = gridDim.x == 1;                      // this block's sums are the call's
-    const float T = m ? (float)m : 1.0f;
     constexpr int PART = CAP > 512 ? 512 : CAP;             // experts per round
-    float b = 0;
 #pragma unroll
     for (int r = 0; r < CAP / PART; ++r) {
         __syncthreads();
@@ -265,38 +318,55 @@ __global__ void __launch_bounds__(ROUTE_BLOCK) route_kernel(RouteArgs a)
             }
         __syncthreads();
         for (int k = threadIdx.x; k < PART; k += ROUTE_BLOCK) {
-            const uint32_t e = r * PART + k;
             float p = 0;
 #pragma unroll
             for (int w = 0; w < WARPS; ++w) p += sums[w][k];
-            if (e < a.experts) {
-                if (alone) {
-                    b += finish_expert(a, e, p, chosen[e], T);
-                } else {
-                    a.part_p[(uint64_t)blockIdx.x * a.experts + e] = p;
-                    a.part_c[(uint64_t)blockIdx.x * a.experts + e] = chosen[e];
-                }
-            }
+            psum[r * PART + k] = p;
         }
     }
-    if (alone) {
+    if (threadIdx.x == 0) { z_block = z; t_block = m; }
+    __syncthreads();
+    if (gridDim.x == 1) {                                   // this block's sums are the call's
+        const float T = m ? (float)m : 1.0f;
+        float b = 0;
+        for (uint32_t e = threadIdx.x; e < a.experts; e += ROUTE_BLOCK) b += finish_expert(a, e, psum[e], chosen[e], T);
         b = lanes_sum<32>(b);
-        __syncthreads();
-        if (lane == 0) zsum[warp] = b;
+        if (lane == 0) bsum[warp] = b;
         __syncthreads();
         if (threadIdx.x == 0) {
             b = 0;
-            for (int w = 0; w < WARPS; ++w) b += zsum[w];
+            for (int w = 0; w < WARPS; ++w) b += bsum[w];
             finish_losses(a, b, z, m, T);
         }
-    } else if (threadIdx.x == 0) {
-        a.part_p[(uint64_t)gridDim.x * a.experts + blockIdx.x] = z;
-        a.part_c[(uint64_t)gridDim.x * a.experts + blockIdx.x] = m;
+        return;
     }
+    // the cluster's sums, each block a fourth of the experts
+    cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
+    cluster.sync();
+    const uint32_t rank = cluster.block_rank(), group = blockIdx.x / ROUTE_CLUSTER, groups = gridDim.x / ROUTE_CLUSTER;
+    for (uint32_t e = rank + ROUTE_CLUSTER * threadIdx.x; e < a.experts; e += ROUTE_CLUSTER * ROUTE_BLOCK) {
+        float p = 0;
+        uint32_t c = 0;
+#pragma unroll
+        for (int r = 0; r < ROUTE_CLUSTER; ++r) {
+            p += *cluster.map_shared_rank(&psum[e], r);
+            c += *cluster.map_shared_rank(&chosen[e], r);
+        }
+        a.part_p[(uint64_t)group * a.experts + e] = p;
+        a.part_c[(uint64_t)group * a.experts + e] = c;
+    }
+    if (rank == 0 && threadIdx.x == 0) {
+        z = 0;
+        m = 0;
+        for (int r = 0; r < ROUTE_CLUSTER; ++r) { z += *cluster.map_shared_rank(&z_block, r); m += *cluster.map_shared_rank(&t_block, r); }
+        a.part_p[(uint64_t)groups * a.experts + group] = z;
+        a.part_c[(uint64_t)groups * a.experts + group] = m;
+    }
+    cluster.sync();                                         // the blocks' shared memory stays until it was read
 }
 
 constexpr int JOIN_BLOCK = 1024, JOIN_CLUSTER = 8;
-// The sums of all blocks: a cluster whose blocks take `width` experts each, JOIN_BLOCK / width threads per expert.
+// The sums of all clusters: a cluster whose blocks take `width` experts each, JOIN_BLOCK / width threads per expert.
 __global__ void __cluster_dims__(JOIN_CLUSTER) __launch_bounds__(JOIN_BLOCK) route_join_kernel(RouteArgs a, uint32_t blocks, uint32_t width)
 {
     __shared__ float sp[JOIN_BLOCK];
@@ -408,7 +478,7 @@ __global__ void __launch_bounds__(ROUTE_BLOCK) route_grad_kernel(RouteGradArgs a
                 c[s] = on && j < a.top ? a.choice[row * a.top + j] : -1;
                 if ((uint32_t)c[s] >= a.experts) c[s] = -1;
                 dw[s] = c[s] >= 0 ? a.dweight[row * a.top + j] : 0.0f;
-                p_c[s] = c[s] >= 0 ? __expf(widen<float>(logits[c[s]]) - lse) : 0.0f;
+                p_c[s] = c[s] >= 0 ? exp2_fast((widen<float>(logits[c[s]]) - lse) * 1.4426950408889634f) : 0.0f;
                 part += dw[s] * p_c[s];
                 kept += p_c[s];
             }
@@ -428,24 +498,24 @@ __global__ void __launch_bounds__(ROUTE_BLOCK) route_grad_kernel(RouteGradArgs a
                 if (c[s] >= 0) atomicAdd(&extra[team][c[s]], p_c[s]);
             __syncwarp();
         }
-        float p[EPT];
-#pragma unroll
-        for (int i = 0; i < EPT; ++i) {
-            p[i] = __expf(x[i] - lse);
-            part += g[i] * p[i];
-        }
+        float p[EPT], along[2] = {0, 0};
+        exponentials<EPT>(x, lse, p);
+        sum_run_of_products<EPT>(along, p, g);
+        part += along[0] + along[1];
         const float off = zf * lse - lanes_sum<TPR>(part);
         if (in) {
 #pragma unroll
             for (int k = 0; k < EPT / VEC; ++k) {
                 const uint32_t e = expert_at<TPR, VEC>(k * VEC, t);
                 if (e < a.experts) {
-                    float d[VEC];
+                    float d[VEC], add[VEC];
 #pragma unroll
-                    for (int j = 0; j < VEC; ++j) {
-                        d[j] = on ? p[k * VEC + j] * (g[k * VEC + j] + off) : 0.0f;
-                        if (a.dweight) d[j] += extra[team][e + j];
-                    }
+                    for (int j = 0; j < VEC; ++j) add[j] = a.dweight ? extra[team][e + j] : 0.0f;
+                    run_add<VEC, true>(d, g + k * VEC, &off);
+                    run_fma<VEC, false, false, false>(d, d, p + k * VEC, add);
+                    if (!on)
+#pragma unroll
+                        for (int j = 0; j < VEC; ++j) d[j] = 0.0f;
                     store_values<X, VEC>((X*)a.dlogits + row * a.dstride + e, d);
                 }
             }
@@ -467,11 +537,13 @@ template <class... KArgs> unsigned resident_blocks(void (*kernel)(KArgs...))
     return n > 0 ? (unsigned)n : 1u;
 }
 
-uint32_t route_teams(uint32_t experts) { return experts <= 16 ? 64 : experts <= 128 ? 32 : 8; }
-// Blocks that leave sums: a rule on the sizes alone, so that the order of the additions is theirs too.
+uint32_t route_teams(uint32_t experts) { return experts <= 16 ? 64 : experts <= 256 ? 32 : experts <= 512 ? 16 : 8; }
+// Blocks at most (launch_clusters may find that fewer fit): a rule on the sizes and the device alone, so that the order of the
+// additions is theirs too.
 unsigned route_blocks(const nups_store* s, uint64_t n, uint32_t experts)
 {
-    return grid_for(n, route_teams(experts), (unsigned)s->sm_count * (experts <= 256 ? 4 : experts <= 512 ? 3 : 2));
+    const unsigned blocks = grid_for(n, route_teams(experts), (unsigned)s->sm_count * (experts <= 64 ? 4 : experts <= 128 ? 3 : 2));
+    return blocks == 1 ? 1 : blocks < ROUTE_CLUSTER ? ROUTE_CLUSTER : blocks / ROUTE_CLUSTER * ROUTE_CLUSTER;       // whole clusters
 }
 
 // Do rows of logits allow runs of VEC?
@@ -480,29 +552,60 @@ bool route_wide(const void* p, uint64_t stride, uint32_t experts, uint64_t n, in
     return experts % vec == 0 && ((uintptr_t)p & (bytes * vec - 1)) == 0 && (n <= 1 || stride % vec == 0);
 }
 
+// Blocks in clusters of ROUTE_CLUSTER, as many as fit on the device at once; a single block by itself.
+cudaError_t launch_clusters(void (*kernel)(RouteArgs), std::atomic<uint32_t>& fit, unsigned& blocks, cudaStream_t st, const RouteArgs& a)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(blocks);
+    cfg.blockDim = dim3(ROUTE_BLOCK);
+    cfg.stream = st;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = ROUTE_CLUSTER;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = blocks == 1 ? 1 : 2;
+    if (blocks > ROUTE_CLUSTER) {                           // asked for once per kernel
+        uint32_t most = fit.load(std::memory_order_relaxed);
+        if (!most) {
+            int n = 0;
+            const cudaError_t e = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
+            if (e != cudaSuccess) return e;
+            most = n > 0 ? (uint32_t)n : 1u;
+            fit.store(most, std::memory_order_relaxed);
+        }
+        if (blocks > most * ROUTE_CLUSTER) blocks = most * ROUTE_CLUSTER;
+        cfg.gridDim = dim3(blocks);
+    }
+    return cudaLaunchKernelEx(&cfg, kernel, a);
+}
+
 template <class X>
 nups_status launch_route(nups_store* s, const RouteArgs& a, cudaStream_t st)
 {
-    const unsigned blocks = route_blocks(s, a.n, a.experts);
+    unsigned blocks = route_blocks(s, a.n, a.experts);
     constexpr int V = 16 / sizeof(X);
     const bool wide = route_wide(a.logits, a.stride, a.experts, a.n, sizeof(X), a.experts <= 16 ? 4 : V);
 #define NUPS_ROUTE(TPR_, EPT_, V_)                                                                                    \
     {                                                                                                                 \
-        if (wide) nups_launch_dependent(route_kernel<X, V_, TPR_, EPT_>, blocks, ROUTE_BLOCK, 0, st, a);              \
-        else nups_launch_dependent(route_kernel<X, 1, TPR_, EPT_>, blocks, ROUTE_BLOCK, 0, st, a);                    \
+        static std::atomic<uint32_t> fit[2];                                                                          \
+        if (wide) CK(launch_clusters(route_kernel<X, V_, TPR_, EPT_>, fit[0], blocks, st, a));                        \
+        else CK(launch_clusters(route_kernel<X, 1, TPR_, EPT_>, fit[1], blocks, st, a));                              \
     }
     if (a.experts <= 16) NUPS_ROUTE(4, 4, 4)
     else if (a.experts <= 64) NUPS_ROUTE(8, 8, V)
     else if (a.experts <= 128) NUPS_ROUTE(8, 16, V)
-    else if (a.experts <= 256) NUPS_ROUTE(32, 8, V)
-    else if (a.experts <= 512) NUPS_ROUTE(32, 16, V)
+    else if (a.experts <= 256) NUPS_ROUTE(8, 32, V)
+    else if (a.experts <= 512) NUPS_ROUTE(16, 32, V)
     else NUPS_ROUTE(32, 32, V)
 #undef NUPS_ROUTE
     LAUNCH_CHECK(s);
     if (blocks == 1) return NUPS_OK;
     uint32_t width = 32;
     while (width * JOIN_CLUSTER < a.experts) width *= 2;
-    nups_launch_dependent(route_join_kernel, JOIN_CLUSTER, JOIN_BLOCK, 0, st, a, blocks, width);
+    nups_launch_dependent(route_join_kernel, JOIN_CLUSTER, JOIN_BLOCK, 0, st, a, blocks / ROUTE_CLUSTER, width);
     LAUNCH_CHECK(s);
     return NUPS_OK;
 }
@@ -523,8 +626,8 @@ nups_status launch_route_grad(nups_store* s, const RouteGradArgs& a, cudaStream_
     if (a.experts <= 16) NUPS_ROUTE(4, 4, 4)
     else if (a.experts <= 64) NUPS_ROUTE(8, 8, V)
     else if (a.experts <= 128) NUPS_ROUTE(8, 16, V)
-    else if (a.experts <= 256) NUPS_ROUTE(32, 8, V)
-    else if (a.experts <= 512) NUPS_ROUTE(32, 16, V)
+    else if (a.experts <= 256) NUPS_ROUTE(8, 32, V)
+    else if (a.experts <= 512) NUPS_ROUTE(16, 32, V)
     else NUPS_ROUTE(32, 32, V)
 #undef NUPS_ROUTE
     LAUNCH_CHECK(s);
@@ -542,8 +645,8 @@ bool route_sizes(int type, uint64_t stride, uint64_t n, uint32_t experts, uint32
 extern "C" nups_status nups_route_scratch(nups_store* s, uint64_t n, uint32_t experts, uint64_t* h_bytes_out)
 {
     if (!s || !h_bytes_out || experts < 1 || experts > NUPS_ROUTE_MAX_EXPERTS || n >= (1ull << 32)) return NUPS_EINVAL;
-    const uint64_t blocks = route_blocks(s, n, experts);
-    *h_bytes_out = blocks > 1 ? blocks * (experts + 1) * 8 : 0;           // one block finishes by itself
+    const uint64_t groups = route_blocks(s, n, experts) / ROUTE_CLUSTER;
+    *h_bytes_out = groups * (experts + 1) * 8;           // one block finishes by itself
     return NUPS_OK;
 }
 
@@ -567,7 +670,7 @@ extern "C" nups_status nups_route(nups_store* s, const void* d_logits, int type,
         if (d_loss) CK(cudaMemsetAsync(d_loss, 0, 3 * sizeof(float), st));
         return NUPS_OK;
     }
-    const uint64_t cells = (uint64_t)route_blocks(s, n, experts) * (experts + 1);
+    const uint64_t cells = (uint64_t)(route_blocks(s, n, experts) / ROUTE_CLUSTER) * (experts + 1);
     RouteArgs a = {d_logits, stride, n, experts, top, d_active, renormalize != 0, d_prob || d_loss, balance, z, d_choice, d_weight, d_lse, d_counts, d_tokens,
                    d_prob, d_loss, (float*)d_scratch, (uint32_t*)d_scratch + cells};
     return type == NUPS_F32 ? launch_route<float>(s, a, st) : type == NUPS_F16 ? launch_route<__half>(s, a, st) : launch_route<__nv_bfloat16>(s, a, st);
