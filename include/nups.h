@@ -436,12 +436,12 @@ nups_status nups_route_scratch(nups_store* store, uint64_t n, uint32_t experts, 
 
 /* The gradient of the logits from that of the loss (d_dloss, one float; NULL: 1)
  * and that of the weights (d_dweight [n][top]; NULL: 0).  Choices and counts are
- * constants.  d_choice, d_lse, d_counts and d_tokens are what nups_route gave for the
- * same arguments.  d_dlogits has the logits' type; items that took no part get 0.
+ * constants.  d_choice, d_weight, d_lse, d_counts and d_tokens are what nups_route gave
+ * for the same arguments (the first two are needed with d_dweight).  d_dlogits has the logits' type; items that took no part get 0.
  * d_dlogits may be d_logits (same stride).                                      */
 nups_status nups_route_grad(nups_store* store, const void* d_logits, int type, uint64_t stride, uint64_t n, uint32_t experts, uint32_t top,
                             const uint8_t* d_active, int renormalize, float balance, float z, const int32_t* d_choice,
-                            const float* d_lse, const uint64_t* d_counts, const uint64_t* d_tokens, const float* d_dloss,
+                            const float* d_weight, const float* d_lse, const uint64_t* d_counts, const uint64_t* d_tokens, const float* d_dloss,
                             const float* d_dweight, void* d_dlogits, uint64_t dlogits_stride, void* stream);
 
 /* Orthogonalized update (Newton-Schulz products): for each of `batch` matrices G of

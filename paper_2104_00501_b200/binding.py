@@ -127,7 +127,7 @@ def load(build_if_missing: bool = True):
         "nups_orthogonalize_scratch": [vp, u32, u32, u32, C.POINTER(u64)],
         "nups_route": [vp, vp, C.c_int, u64, u64, u32, u32, vp, C.c_int, f32, f32, vp, vp, vp, vp, vp, vp, vp, vp, u64, vp],
         "nups_route_scratch": [vp, u64, u32, C.POINTER(u64)],
-        "nups_route_grad": [vp, vp, C.c_int, u64, u64, u32, u32, vp, C.c_int, f32, f32, vp, vp, vp, vp, vp, vp, vp, u64, vp],
+        "nups_route_grad": [vp, vp, C.c_int, u64, u64, u32, u32, vp, C.c_int, f32, f32, vp, vp, vp, vp, vp, vp, vp, vp, u64, vp],
     }
     for name, args in sig.items():
         fn = getattr(L, name)
@@ -580,42 +580,20 @@ class Store:
         p, stride = self._rows(w, logits)
         n, experts = logits.shape
         po, os_ = self._rows(w, out, n, experts)
-        top = r.choice.shape[1]
-        if out.dtype != logits.dtype or tuple(r.choice.shape) != (n, top) or r.counts.numel() != experts:
+        top, pdw = r.choice.shape[1], None
+        if out.dtype != logits.dtype or r.choice.shape[0] != n or r.lse.shape[0] != n or r.counts.shape[0] != experts:
             raise NupsError(EINVAL, w, "out must have the logits' type, and the routing must be of these logits")
-        if dweight is not None and (tuple(dweight.shape) != (n, top) or dweight.dtype != torch.float32 or not dweight.is_contiguous()):
-            raise NupsError(EINVAL, w, f"dweight must be a contiguous float32 {n} x {top}")
+        if r.counts.dtype != torch.int64 or r.tokens.dtype != torch.int64 or not (r.counts.is_cuda and r.tokens.is_cuda):
+            raise NupsError(EINVAL, w, "counts and tokens must be int64, on the store's device")
+        if dweight is not None:
+            if dweight.shape != r.choice.shape or dweight.dtype != torch.float32 or not dweight.is_contiguous():
+                raise NupsError(EINVAL, w, f"dweight must be a contiguous float32 {n} x {top}")
+            pdw = dweight.data_ptr()
         if dloss is not None and (dloss.numel() != 1 or dloss.dtype != torch.float32):
             raise NupsError(EINVAL, w, "dloss must be one float32")
-        self._chk(self._l.nups_route_grad(self._s, p, _type(logits), stride, n, experts, top, self._active(w, r.active, n), int(r.renormalize), r.balance,
-                                          r.z, _ptr(r.choice), self._vector(w, r.lse, n), _ptr(r.counts, torch.int64), _ptr(r.tokens, torch.int64),
-                                          _ptr(dloss), _ptr(dweight), po, os_, _stream()), w)
-        return out
-
-    def orthogonalize(self, update, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7, scale=1.0, out=None):
-        """`scale` times the Newton-Schulz iterate of a matrix [rows, cols] or of a batch of them [batch, rows, cols]; out may be
-        the update itself.  What push adds to rows that hold matrices: scale = -rate, out as [batch, rows * cols]."""
-        w = "nups_orthogonalize"
-        if out is None:
-            out = torch.empty_like(update, memory_format=torch.contiguous_format)
-        self._on_device(w, update, out)
-        if update.dim() not in (2, 3) or out.shape != update.shape or out.dtype != update.dtype or len(coefficients) != 3:
-            raise NupsError(EINVAL, w, "expected a matrix or a batch of them, out of the same shape and type, three coefficients")
-        (batch, rows, cols), places = (1,) * (3 - update.dim()) + tuple(update.shape), []
-        for t in (update, out):
-            if cols > 1 and t.stride(-1) != 1:
-                raise NupsError(EINVAL, w, "the values of a row must be contiguous")
-            places.append((t.data_ptr(), t.stride(-2) if rows > 1 else cols, t.stride(0) if batch > 1 and t.dim() == 3 else 0))
-            if places[-1][1] < 0 or places[-1][2] < 0:
-                raise NupsError(EINVAL, w, "strides must not be negative")
-        size = self._scratch_bytes("nups_orthogonalize_scratch", batch, rows, cols)
-        (pg, gs, gb), (po, os_, ob) = places
-        stream, kind = _stream(), _type(update)
-        scratch = _scratch_alloc(size, stream) if size else None
-        rc = self._l.nups_orthogonalize(self._s, pg, kind, gs, gb, batch, rows, cols, steps, (C.c_float * 3)(*coefficients), eps, scale, po, os_, ob,
-                                        scratch, size, stream)
-        if scratch:
-            _scratch_free(scratch)
+        rc = self._l.nups_route_grad(self._s, p, _type(logits), stride, n, experts, top, self._active(w, r.active, n), r.renormalize, r.balance, r.z,
+                                     r.choice.data_ptr(), r.weight.data_ptr(), r.lse.data_ptr(), r.counts.data_ptr(), r.tokens.data_ptr(),
+                                     None if dloss is None else dloss.data_ptr(), pdw, po, os_, _stream())
         if rc:
             self._chk(rc, w)
         return out

@@ -72,7 +72,12 @@ __device__ __forceinline__ uint32_t ordered(float x)
 __device__ __forceinline__ float from_ordered(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u); }
 // fp16 and bf16 leave at least 13 bits of a float's mantissa free: the larger number there is the lower expert
 constexpr uint32_t FREE = 0x1FFFu;
-__device__ __forceinline__ uint32_t ordered_with(float x, uint32_t e) { return (ordered(x) & ~FREE) | (FREE - e); }
+// tag = 0x80000000 | (FREE - e): the free bits of x are zero, so the key is two operations on the number's bits
+__device__ __forceinline__ uint32_t ordered_with(float x, uint32_t tag)
+{
+    const uint32_t b = __float_as_uint(x + 0.0f);
+    return b ^ ((uint32_t)((int32_t)b >> 31) & (0x7FFFFFFFu & ~FREE)) ^ tag;
+}
 __device__ __forceinline__ float logit_of(uint32_t key) { return from_ordered(key & 0x80000000u ? key & ~FREE : key | FREE); }
 
 // The largest keys of a lane, in order, each with its expert (PACKED: in the key).
@@ -128,15 +133,23 @@ template <int TPR, int VEC> __device__ __forceinline__ uint32_t expert_at(int i,
     return (uint32_t)(((i / VEC) * TPR + t) * VEC + i % VEC);
 }
 
+// A lane's logits as they lie in memory, and as floats (-infinity where there is none).
 template <class X, int VEC, int TPR, int EPT>
-__device__ __forceinline__ void load_logits(const X* row, bool in, uint32_t experts, int t, float fill, float (&x)[EPT])
+__device__ __forceinline__ void fetch_logits(const X* row, bool in, uint32_t experts, int t, Pack<X, VEC> (&raw)[EPT / VEC])
+{
+#pragma unroll
+    for (int c = 0; c < EPT / VEC; ++c)
+        if (in && expert_at<TPR, VEC>(c * VEC, t) < experts) raw[c] = load_pack<X, VEC>(row + expert_at<TPR, VEC>(c * VEC, t));
+}
+template <class X, int VEC, int TPR, int EPT>
+__device__ __forceinline__ void read_logits(const Pack<X, VEC> (&raw)[EPT / VEC], bool in, uint32_t experts, int t, float (&x)[EPT])
 {
 #pragma unroll
     for (int c = 0; c < EPT / VEC; ++c) {
-        const uint32_t e = expert_at<TPR, VEC>(c * VEC, t);
+        if (in && expert_at<TPR, VEC>(c * VEC, t) < experts) unpack<float>(raw[c], x + c * VEC);
+        else
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) x[c * VEC + j] = fill;
-        if (in && e < experts) unpack<float>(load_pack<X, VEC>(row + e), x + c * VEC);
+            for (int j = 0; j < VEC; ++j) x[c * VEC + j] = -CUDART_INF_F;
     }
 }
 
@@ -160,7 +173,7 @@ __device__ __forceinline__ void finish_losses(const RouteArgs& a, float b, float
 }
 
 // e^(x - most), elementwise
-template <int EPT> __device__ __forceinline__ void exponentials(const float (&x)[EPT], float most, float (&ex)[EPT])
+template <int EPT> __device__ __forceinline__ void exponentials(const float* x, float most, float* ex)
 {
     const float minus = -most, log2e = 1.4426950408889634f;
     run_add<EPT, true>(ex, x, &minus);
@@ -169,12 +182,11 @@ template <int EPT> __device__ __forceinline__ void exponentials(const float (&x)
     for (int i = 0; i < EPT; ++i) ex[i] = exp2_fast(ex[i]);
 }
 
-template <class X, int VEC, int TPR, int EPT>
+template <class X, int VEC, int TPR, int EPT, int KEPT>
 __global__ void __launch_bounds__(ROUTE_BLOCK, EPT <= 8 ? 4 : EPT <= 16 ? 3 : 2) route_kernel(RouteArgs a)
 {
     constexpr int TEAMS = ROUTE_BLOCK / TPR, CAP = TPR * EPT, SLOTS = route_slots(TPR), WARPS = ROUTE_BLOCK / 32;
     constexpr bool PACKED = sizeof(X) == 2;
-    constexpr int KEPT = PACKED ? (EPT < 8 ? 2 : 4) : 2;
     __shared__ uint32_t chosen[CAP];                        // counts of this block
     __shared__ float sums[WARPS][CAP > 512 ? 512 : CAP];
     __shared__ float psum[CAP];
@@ -190,17 +202,21 @@ __global__ void __launch_bounds__(ROUTE_BLOCK, EPT <= 8 ? 4 : EPT <= 16 ? 3 : 2)
     uint32_t items = 0;
 #pragma unroll
     for (int i = 0; i < EPT; ++i) acc[i] = 0;
-    for (uint64_t base = (uint64_t)blockIdx.x * TEAMS; base < a.n; base += (uint64_t)gridDim.x * TEAMS) {
-        const uint64_t row = base + team;
+    const uint64_t step = (uint64_t)gridDim.x * TEAMS;
+    uint64_t row = (uint64_t)blockIdx.x * TEAMS + team;
+    const uint32_t tag = 0x80000000u | (FREE ^ (uint32_t)(t * VEC));      // of the lane's first expert; the others differ in other bits
+    for (uint64_t base = (uint64_t)blockIdx.x * TEAMS; base < a.n; base += step, row += step) {
         const bool in = row < a.n;
         bool on = in && (!a.active || a.active[row]);
-        float x[EPT], ex[EPT], total, most;
-        load_logits<X, VEC, TPR, EPT>((const X*)a.logits + row * a.stride, on, a.experts, t, -CUDART_INF_F, x);
+        float x[EPT], total, most;                          // logits, then their exponentials
+        Pack<X, VEC> raw[EPT / VEC];
+        fetch_logits<X, VEC, TPR, EPT>((const X*)a.logits + row * a.stride, in, a.experts, t, raw);       // does not wait for the mask
+        read_logits<X, VEC, TPR, EPT>(raw, on, a.experts, t, x);
         uint32_t slot_u[SLOTS];
         int32_t slot_e[SLOTS];
-        bool any, again = false;
-        auto key_of = [&](int i) { return PACKED ? ordered_with(x[i], expert_at<TPR, VEC>(i, t)) : ordered(x[i]); };
-        do {
+        bool any, nan_item = false;
+        auto key_of = [&](int i) { return PACKED ? ordered_with(x[i], tag ^ expert_at<TPR, VEC>(i, 0)) : ordered(x[i]); };
+        for (int pass = 0;; ++pass) {
             Largest<PACKED, KEPT> top;
             int left = 0;                                   // of those kept
             uint32_t u = 0xFFFFFFFFu, e = 0;                // the last one chosen
@@ -239,22 +255,24 @@ __global__ void __launch_bounds__(ROUTE_BLOCK, EPT <= 8 ? 4 : EPT <= 16 ? 3 : 2)
                     if (t == l && some) { slot_u[s] = u; slot_e[s] = (int32_t)e; }
                 }
             }
-            exponentials<EPT>(x, most, ex);
+            exponentials<EPT>(x, most, x);
             float two_sums[2] = {0, 0};
-            sum_run<EPT>(two_sums, ex);
+            sum_run<EPT>(two_sums, x);
             total = lanes_sum<TPR>(two_sums[0] + two_sums[1]);
-            // NaN: the order above is void.  Once more without the NaN, which then are not chosen; the item's sum stays NaN.
-            if (again) total = CUDART_NAN_F;
-            again = !again && total != total;
-            bool nan_here = false;
-#pragma unroll
-            for (int i = 0; i < EPT; ++i) {
-                nan_here = nan_here || x[i] != x[i];
-                if (again && x[i] != x[i]) x[i] = -CUDART_INF_F;
+            if (pass == 1) {
+                if (nan_item) total = CUDART_NAN_F;
+                break;
             }
-            const bool nan_there = lanes_max<TPR>(nan_here ? 1u : 0u) != 0;       // by all lanes of the warp
-            again = again && nan_there;                     // +infinity does it too, and is in order
-        } while (__any_sync(0xFFFFFFFFu, again));
+            nan_item = total != total;
+            if (!__any_sync(0xFFFFFFFFu, nan_item)) break;
+            // NaN, which the order above knows nothing of (or +infinity): once more with NaN as what is not chosen; the item's
+            // sum stays NaN
+            fetch_logits<X, VEC, TPR, EPT>((const X*)a.logits + row * a.stride, on, a.experts, t, raw);
+            read_logits<X, VEC, TPR, EPT>(raw, on, a.experts, t, x);
+#pragma unroll
+            for (int i = 0; i < EPT; ++i)
+                if (x[i] != x[i]) x[i] = -CUDART_INF_F;
+        }
         if (!any && total == 0.0f) on = false;              // nothing but -infinity
         const float inv = on ? 1.0f / total : 0.0f;
         float kept[SLOTS], kept_sum = 0;
@@ -287,7 +305,7 @@ __global__ void __launch_bounds__(ROUTE_BLOCK, EPT <= 8 ? 4 : EPT <= 16 ? 3 : 2)
                 zacc += lse * lse;
                 ++items;
             }
-            if (a.sums) run_fma<EPT, false, true, false>(acc, ex, &inv, acc);
+            if (a.sums) run_fma<EPT, false, true, false>(acc, x, &inv, acc);
         } else if (in && t == 0 && a.lse) {
             a.lse[row] = 0.0f;
         }
@@ -432,7 +450,7 @@ struct RouteGradArgs {
     int renormalize;
     float balance, z;
     const int32_t* choice;
-    const float* lse;
+    const float *weight, *lse;
     const uint64_t *counts, *tokens;
     const float *dloss, *dweight;
     void* dlogits;
@@ -461,45 +479,47 @@ __global__ void __launch_bounds__(ROUTE_BLOCK) route_grad_kernel(RouteGradArgs a
         g[i] = e < a.experts ? bf * (float)a.counts[e] : 0.0f;
     }
     __syncwarp();
-    for (uint64_t base = (uint64_t)blockIdx.x * TEAMS; base < a.n; base += (uint64_t)gridDim.x * TEAMS) {
-        const uint64_t row = base + team;
-        const bool in = row < a.n;
-        const bool on = in && (!a.active || a.active[row]);
-        const X* logits = (const X*)a.logits + row * a.stride;
-        const float lse = on ? a.lse[row] : 0.0f;
-        float x[EPT];
-        load_logits<X, VEC, TPR, EPT>(logits, on, a.experts, t, -CUDART_INF_F, x);
+    const uint64_t step = (uint64_t)gridDim.x * TEAMS;
+    uint64_t row = (uint64_t)blockIdx.x * TEAMS + team;
+    for (uint64_t base = (uint64_t)blockIdx.x * TEAMS; base < a.n; base += step, row += step) {
+        const bool in = row < a.n, on = in && (!a.active || a.active[row]);
+        Pack<X, VEC> raw[EPT / VEC];
+        fetch_logits<X, VEC, TPR, EPT>((const X*)a.logits + row * a.stride, in, a.experts, t, raw);       // nothing waits for the mask
+        const float lse = in ? a.lse[row] : 0.0f;
         int32_t c[SLOTS];
-        float p_c[SLOTS], dw[SLOTS], part = 0, kept = 0;
+        float add[SLOTS], dw[SLOTS], part = 0;
         if (a.dweight) {
 #pragma unroll
             for (int s = 0; s < SLOTS; ++s) {
                 const uint32_t j = s * TPR + t;
-                c[s] = on && j < a.top ? a.choice[row * a.top + j] : -1;
-                if ((uint32_t)c[s] >= a.experts) c[s] = -1;
-                dw[s] = c[s] >= 0 ? a.dweight[row * a.top + j] : 0.0f;
-                p_c[s] = c[s] >= 0 ? exp2_fast((widen<float>(logits[c[s]]) - lse) * 1.4426950408889634f) : 0.0f;
-                part += dw[s] * p_c[s];
-                kept += p_c[s];
+                const bool has = in && j < a.top;
+                c[s] = has ? a.choice[row * a.top + j] : -1;
+                add[s] = has ? a.weight[row * a.top + j] : 0.0f;
+                dw[s] = has ? a.dweight[row * a.top + j] : 0.0f;
             }
-            if (a.renormalize) {
-                kept = lanes_sum<TPR>(kept);
-                const float inv = kept != 0.0f ? 1.0f / kept : 0.0f;
-                const float mean = lanes_sum<TPR>(part) * inv;
+#pragma unroll
+            for (int s = 0; s < SLOTS; ++s) {
+                if (!on || (uint32_t)c[s] >= a.experts) { c[s] = -1; add[s] = dw[s] = 0.0f; }
+                part += dw[s] * add[s];
+            }
+            if (a.renormalize) {                            // w (dweight - sum dweight w)
+                const float mean = lanes_sum<TPR>(part);
                 part = 0.0f;
 #pragma unroll
-                for (int s = 0; s < SLOTS; ++s) p_c[s] *= inv * (dw[s] - mean);
-            } else {
+                for (int s = 0; s < SLOTS; ++s) add[s] *= dw[s] - mean;
+            } else {                                        // p dweight; the sum takes part in sum g p
 #pragma unroll
-                for (int s = 0; s < SLOTS; ++s) p_c[s] *= dw[s];
+                for (int s = 0; s < SLOTS; ++s) add[s] *= dw[s];
             }
 #pragma unroll
             for (int s = 0; s < SLOTS; ++s)
-                if (c[s] >= 0) atomicAdd(&extra[team][c[s]], p_c[s]);
+                if (c[s] >= 0) atomicAdd(&extra[team][c[s]], add[s]);
             __syncwarp();
         }
-        float p[EPT], along[2] = {0, 0};
-        exponentials<EPT>(x, lse, p);
+        float p[EPT];                                       // logits, then probabilities
+        read_logits<X, VEC, TPR, EPT>(raw, on, a.experts, t, p);
+        float along[2] = {0, 0};
+        exponentials<EPT>(p, lse, p);
         sum_run_of_products<EPT>(along, p, g);
         part += along[0] + along[1];
         const float off = zf * lse - lanes_sum<TPR>(part);
@@ -508,11 +528,11 @@ __global__ void __launch_bounds__(ROUTE_BLOCK) route_grad_kernel(RouteGradArgs a
             for (int k = 0; k < EPT / VEC; ++k) {
                 const uint32_t e = expert_at<TPR, VEC>(k * VEC, t);
                 if (e < a.experts) {
-                    float d[VEC], add[VEC];
+                    float d[VEC], more[VEC];
 #pragma unroll
-                    for (int j = 0; j < VEC; ++j) add[j] = a.dweight ? extra[team][e + j] : 0.0f;
+                    for (int j = 0; j < VEC; ++j) more[j] = a.dweight ? extra[team][e + j] : 0.0f;
                     run_add<VEC, true>(d, g + k * VEC, &off);
-                    run_fma<VEC, false, false, false>(d, d, p + k * VEC, add);
+                    run_fma<VEC, false, false, false>(d, d, p + k * VEC, more);
                     if (!on)
 #pragma unroll
                         for (int j = 0; j < VEC; ++j) d[j] = 0.0f;
@@ -537,12 +557,12 @@ template <class... KArgs> unsigned resident_blocks(void (*kernel)(KArgs...))
     return n > 0 ? (unsigned)n : 1u;
 }
 
-uint32_t route_teams(uint32_t experts) { return experts <= 16 ? 64 : experts <= 256 ? 32 : experts <= 512 ? 16 : 8; }
+uint32_t route_teams(uint32_t experts) { return experts <= 16 ? 64 : experts <= 128 ? 32 : experts <= 256 ? 16 : 8; }      // at least
 // Blocks at most (launch_clusters may find that fewer fit): a rule on the sizes and the device alone, so that the order of the
 // additions is theirs too.
 unsigned route_blocks(const nups_store* s, uint64_t n, uint32_t experts)
 {
-    const unsigned blocks = grid_for(n, route_teams(experts), (unsigned)s->sm_count * (experts <= 64 ? 4 : experts <= 128 ? 3 : 2));
+    const unsigned blocks = grid_for(n, route_teams(experts), (unsigned)s->sm_count * (experts <= 64 ? 4 : experts <= 512 ? 3 : 2));
     return blocks == 1 ? 1 : blocks < ROUTE_CLUSTER ? ROUTE_CLUSTER : blocks / ROUTE_CLUSTER * ROUTE_CLUSTER;       // whole clusters
 }
 
@@ -588,19 +608,27 @@ nups_status launch_route(nups_store* s, const RouteArgs& a, cudaStream_t st)
     unsigned blocks = route_blocks(s, a.n, a.experts);
     constexpr int V = 16 / sizeof(X);
     const bool wide = route_wide(a.logits, a.stride, a.experts, a.n, sizeof(X), a.experts <= 16 ? 4 : V);
-#define NUPS_ROUTE(TPR_, EPT_, V_)                                                                                    \
+    // KEPT: as many as a lane is at all likely to give (a lane that gives more looks through its logits again)
+#define NUPS_ROUTE_KEPT(TPR_, EPT_, V_, KEPT_)                                                                        \
     {                                                                                                                 \
         static std::atomic<uint32_t> fit[2];                                                                          \
-        if (wide) CK(launch_clusters(route_kernel<X, V_, TPR_, EPT_>, fit[0], blocks, st, a));                        \
-        else CK(launch_clusters(route_kernel<X, 1, TPR_, EPT_>, fit[1], blocks, st, a));                              \
+        if (wide) CK(launch_clusters(route_kernel<X, V_, TPR_, EPT_, KEPT_>, fit[0], blocks, st, a));                 \
+        else CK(launch_clusters(route_kernel<X, 1, TPR_, EPT_, KEPT_>, fit[1], blocks, st, a));                       \
+    }
+#define NUPS_ROUTE(TPR_, EPT_, V_)                                                                                    \
+    {                                                                                                                 \
+        if (a.top == 1) NUPS_ROUTE_KEPT(TPR_, EPT_, V_, 1)                                                            \
+        else if (a.top <= 2 || sizeof(X) == 4 || EPT_ < 8) NUPS_ROUTE_KEPT(TPR_, EPT_, V_, 2)                         \
+        else if constexpr (sizeof(X) == 2 && EPT_ >= 8) NUPS_ROUTE_KEPT(TPR_, EPT_, V_, 4)                            \
     }
     if (a.experts <= 16) NUPS_ROUTE(4, 4, 4)
     else if (a.experts <= 64) NUPS_ROUTE(8, 8, V)
     else if (a.experts <= 128) NUPS_ROUTE(8, 16, V)
-    else if (a.experts <= 256) NUPS_ROUTE(8, 32, V)
-    else if (a.experts <= 512) NUPS_ROUTE(16, 32, V)
+    else if (a.experts <= 256) NUPS_ROUTE((sizeof(X) == 2 ? 8 : 16), (sizeof(X) == 2 ? 32 : 16), V)
+    else if (a.experts <= 512) NUPS_ROUTE((sizeof(X) == 2 ? 16 : 32), (sizeof(X) == 2 ? 32 : 16), V)
     else NUPS_ROUTE(32, 32, V)
 #undef NUPS_ROUTE
+#undef NUPS_ROUTE_KEPT
     LAUNCH_CHECK(s);
     if (blocks == 1) return NUPS_OK;
     uint32_t width = 32;
@@ -626,8 +654,8 @@ nups_status launch_route_grad(nups_store* s, const RouteGradArgs& a, cudaStream_
     if (a.experts <= 16) NUPS_ROUTE(4, 4, 4)
     else if (a.experts <= 64) NUPS_ROUTE(8, 8, V)
     else if (a.experts <= 128) NUPS_ROUTE(8, 16, V)
-    else if (a.experts <= 256) NUPS_ROUTE(8, 32, V)
-    else if (a.experts <= 512) NUPS_ROUTE(16, 32, V)
+    else if (a.experts <= 256) NUPS_ROUTE((sizeof(X) == 2 ? 8 : 16), (sizeof(X) == 2 ? 32 : 16), V)
+    else if (a.experts <= 512) NUPS_ROUTE((sizeof(X) == 2 ? 16 : 32), (sizeof(X) == 2 ? 32 : 16), V)
     else NUPS_ROUTE(32, 32, V)
 #undef NUPS_ROUTE
     LAUNCH_CHECK(s);
@@ -678,14 +706,14 @@ extern "C" nups_status nups_route(nups_store* s, const void* d_logits, int type,
 
 extern "C" nups_status nups_route_grad(nups_store* s, const void* d_logits, int type, uint64_t stride, uint64_t n, uint32_t experts, uint32_t top,
                                        const uint8_t* d_active, int renormalize, float balance, float z, const int32_t* d_choice,
-                                       const float* d_lse, const uint64_t* d_counts, const uint64_t* d_tokens, const float* d_dloss,
+                                       const float* d_weight, const float* d_lse, const uint64_t* d_counts, const uint64_t* d_tokens, const float* d_dloss,
                                        const float* d_dweight, void* d_dlogits, uint64_t dlogits_stride, void* stream)
 {
     if (!s || !route_sizes(type, stride, n, experts, top, balance, z) || !route_sizes(type, dlogits_stride, n, experts, top, 0, 0)) return NUPS_EINVAL;
-    if (n && (!d_logits || !d_lse || !d_counts || !d_tokens || !d_dlogits || (d_dweight && !d_choice))) return NUPS_EINVAL;
+    if (n && (!d_logits || !d_lse || !d_counts || !d_tokens || !d_dlogits || (d_dweight && (!d_choice || !d_weight)))) return NUPS_EINVAL;
     nups_status rc = on_own_device(s);
     if (rc != NUPS_OK || n == 0) return rc;
-    RouteGradArgs a = {d_logits, stride, n, experts, top, d_active, renormalize != 0, balance, z, d_choice, d_lse, d_counts, d_tokens, d_dloss, d_dweight,
+    RouteGradArgs a = {d_logits, stride, n, experts, top, d_active, renormalize != 0, balance, z, d_choice, d_weight, d_lse, d_counts, d_tokens, d_dloss, d_dweight,
                        d_dlogits, dlogits_stride};
     cudaStream_t st = (cudaStream_t)stream;
     return type == NUPS_F32 ? launch_route_grad<float>(s, a, st)
