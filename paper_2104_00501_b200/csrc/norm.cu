@@ -636,6 +636,7 @@ struct GradArgs {
     uint64_t n;
     uint32_t len;
     int dy_type, w_type, w_vec;
+    DevStat* st;
 };
 
 // One pass: a team holds x and dy of ROWS rows in registers and, over all of its rows, its columns' shares of dweight and dbias
@@ -809,6 +810,144 @@ __global__ void __launch_bounds__(team_block(TPR)) norm_grad_kernel(GradArgs a)
     }
 }
 
+// Rows above 1 KB: x and dy come through a ring in shared memory, as in norm_ring_kernel, and are read there twice.
+// (16,384 rows of 4096 bf16: 90 us with the rows in registers.)
+template <class X, class D, int TPR, int CH, int ROWS, int STAGES>
+__global__ void __launch_bounds__(TPR) norm_grad_ring_kernel(GradArgs a)
+{
+    typedef typename Acc<X>::type A;
+    constexpr int VEC = 16 / sizeof(X), WARPS = TPR / 32;
+    extern __shared__ __align__(128) char ring[];
+    __shared__ A shared[4 * ROWS * WARPS];
+    __shared__ uint64_t bars[STAGES];
+    const int t = threadIdx.x;
+    const uint32_t x_bytes = a.len * sizeof(X), d_bytes = a.len * sizeof(D), stage_bytes = (x_bytes + d_bytes) * ROWS;
+    const uint64_t step = (uint64_t)gridDim.x * ROWS, first = (uint64_t)blockIdx.x * ROWS;
+    auto bar = [&](uint32_t s) { return smem_address(&bars[s]); };
+    if (t == 0) {
+        for (int s = 0; s < STAGES; ++s) mbar_init(bar(s), 1);
+        mbar_init_visible();
+    }
+    grid_dependency_wait();
+    auto issue = [&](uint32_t i) {                          // the block's group i; one thread
+        const uint64_t base = first + i * step;
+        if (base >= a.n) return;
+        const uint32_t rows = (uint32_t)min((uint64_t)ROWS, a.n - base), s = i % STAGES, to = smem_address(ring) + s * stage_bytes, to_d = to + ROWS * x_bytes;
+        mbar_expect(bar(s), rows * (x_bytes + d_bytes));
+        if (a.xs == a.len) bulk_load(to, (const X*)a.x + base * a.xs, rows * x_bytes, bar(s));
+        else
+            for (uint32_t k = 0; k < rows; ++k) bulk_load(to + k * x_bytes, (const X*)a.x + (base + k) * a.xs, x_bytes, bar(s));
+        if (a.dys == a.len) bulk_load(to_d, (const D*)a.dy + base * a.dys, rows * d_bytes, bar(s));
+        else
+            for (uint32_t k = 0; k < rows; ++k) bulk_load(to_d + k * d_bytes, (const D*)a.dy + (base + k) * a.dys, d_bytes, bar(s));
+    };
+    if (t == 0)
+        for (uint32_t i = 0; i + 1 < STAGES; ++i) issue(i);
+    A w[CH][VEC], dw[CH][VEC], db[CH][VEC];
+    load_params<X, A, VEC, TPR, CH>(a.w, a.w_type, a.w_vec, a.len, t, (A)1, w);
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) dw[c][j] = db[c][j] = 0;
+    const A inv_len = (A)1 / (A)a.len;
+    __syncthreads();                                        // the barriers are there
+    uint32_t i = 0;
+    bool ok = true;
+    for (uint64_t base = first; base < a.n; base += step, ++i) {
+        const uint32_t s = i % STAGES;
+        const X* x = (const X*)(ring + s * stage_bytes);
+        const D* dy = (const D*)(ring + s * stage_bytes + ROWS * x_bytes);
+        A mean[ROWS], rstd[ROWS], s1[ROWS], s2[ROWS];
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) {
+            mean[k] = base + k < a.n ? ((const A*)a.mean)[base + k] : (A)0;
+            rstd[k] = base + k < a.n ? ((const A*)a.rstd)[base + k] : (A)0;
+        }
+        ok = mbar_wait(bar(s), (i / STAGES) & 1);
+        auto hat = [&](int k, uint32_t at, A* h, A* d) {
+            const A minus = -mean[k];
+            unpack<A>(load_pack<X, VEC>(x + k * a.len + at), h);
+            unpack<A>(load_pack<D, VEC>(dy + k * a.len + at), d);
+            run_add<VEC, true>(h, h, &minus);
+            run_scale<VEC>(h, h, rstd[k]);
+        };
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) {
+            A a1[2] = {0, 0}, a2[2] = {0, 0};
+            if (base + k < a.n)                             // the same for the whole block
+#pragma unroll
+                for (int c = 0; c < CH; ++c) {
+                    const uint32_t at = value_at<TPR, VEC>(c, t);
+                    if (at < a.len) {
+                        A h[VEC], d[VEC];
+                        hat(k, at, h, d);
+                        run_fma<VEC, false, false, false>(dw[c], d, h, dw[c]);
+                        run_add<VEC, false>(db[c], db[c], d);
+                        run_mul<VEC>(d, d, w[c]);
+                        sum_run<VEC>(a1, d);
+                        sum_run_of_products<VEC>(a2, d, h);
+                    }
+                }
+            s1[k] = a1[0] + a1[1];
+            s2[k] = a2[0] + a2[1];
+        }
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) {
+            s1[k] = team_sum<32>(s1[k]);
+            s2[k] = team_sum<32>(s2[k]);
+        }
+        A* st = shared + (i & 1) * 2 * ROWS * WARPS;
+        const int lane = t & 31;
+        if (lane == 0)
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k) { st[k * WARPS + (t >> 5)] = s1[k]; st[(ROWS + k) * WARPS + (t >> 5)] = s2[k]; }
+        if (__syncthreads_or(!ok)) { ok = false; break; }
+        if (t == 0) issue(i + STAGES - 1);                  // every thread is done with the group before this one
+        if (!a.dx) continue;
+        constexpr int AT_ONCE = 32 / WARPS < 2 * ROWS ? 32 / WARPS : 2 * ROWS;
+#pragma unroll
+        for (int i0 = 0; i0 < 2 * ROWS; i0 += AT_ONCE) {
+            const A sum = team_sum<WARPS>(st[(i0 + (lane / WARPS) % AT_ONCE) * WARPS + lane % WARPS]);
+#pragma unroll
+            for (int q = 0; q < AT_ONCE; ++q) {
+                const A r = __shfl_sync(0xFFFFFFFFu, sum, q * WARPS);
+                if (i0 + q < ROWS) s1[i0 + q] = r;
+                else s2[i0 + q - ROWS] = r;
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const uint32_t at = value_at<TPR, VEC>(c, t);
+            if (at < a.len)
+#pragma unroll
+                for (int k = 0; k < ROWS; ++k) {
+                    const A m1 = -s1[k] * inv_len * rstd[k], m2 = -s2[k] * inv_len * rstd[k];
+                    A h[VEC], d[VEC];
+                    hat(k, at, h, d);
+                    run_mul<VEC>(d, d, w[c]);
+                    run_fma<VEC, false, true, true>(h, h, &m2, &m1);
+                    run_fma<VEC, false, true, false>(d, d, &rstd[k], h);
+                    if (base + k < a.n) store_values<X, VEC>((X*)a.dx + (base + k) * a.dxs + at, d);
+                }
+        }
+    }
+    if (!ok) {                                              // a copy did not come: say so, and leave none in flight
+        atomicCAS(&a.st->status, 0, NUPS_ETIMEOUT);
+        if (t == 0)
+            for (uint32_t k = i + 1; k < i + STAGES - 1; ++k)
+                if (first + k * step < a.n) mbar_wait(bar(k % STAGES), (k / STAGES) & 1);
+    }
+    if (!a.part) return;
+    A* out = (A*)a.part + (uint64_t)blockIdx.x * 2 * a.len;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const uint32_t at = value_at<TPR, VEC>(c, t);
+        if (at < a.len)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) { out[at + j] = dw[c][j]; out[a.len + at + j] = db[c][j]; }
+    }
+}
+
 // Rows too long for registers, first pass: a block per row leaves mean(g) and mean(g h).
 template <class X, int VEC>
 __global__ void __launch_bounds__(1024) norm_grad_sums_kernel(GradArgs a, typename Acc<X>::type* sums)
@@ -922,7 +1061,31 @@ nups_status launch_grad(nups_store* s, GradArgs a, int x_type, void* d_dw, void*
         if (smem > 48 * 1024) CK(cudaFuncSetAttribute(norm_grad_kernel<X, D, VEC, TPR_, CH_, ROWS_>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)); \
         nups_launch_dependent(norm_grad_kernel<X, D, VEC, TPR_, CH_, ROWS_>, blocks, team_block(TPR_), smem, st, a);      \
     }
-    if (len > grad_long_from(x_type)) {
+#define NUPS_GRAD_RING(TPR_, CH_, ROWS_, STAGES_)                                                                                           \
+    {                                                                                                                                      \
+        const size_t smem = (size_t)STAGES_ * ROWS_ * len * (sizeof(X) + sizeof(D));                                                       \
+        static std::atomic<uint64_t> last{0};                                                                                              \
+        if (!ring_blocks(last, s->device, norm_grad_ring_kernel<X, D, TPR_, CH_, ROWS_, STAGES_>, TPR_, smem))                             \
+            return nups_cuda_fail(cudaGetLastError(), "norm_grad_ring_kernel");                                                            \
+        nups_launch_dependent(norm_grad_ring_kernel<X, D, TPR_, CH_, ROWS_, STAGES_>, blocks, TPR_, smem, st, a);                          \
+    }
+    bool through_ring = false;
+    if constexpr (VEC > 1) {
+        // fewer rows: every block has one group, nothing to run ahead of
+        through_ring = chunks > 64 && chunks <= (sizeof(X) == 2 ? 1024 : 2048) && a.n > (uint64_t)s->sm_count && len * sizeof(D) % 16 == 0 && ((uintptr_t)a.dy & 15) == 0 &&
+                       a.dys * sizeof(D) % 16 == 0;
+        if (through_ring) {
+            if (chunks <= 128) NUPS_GRAD_RING(128, 1, 4, 3)
+            else if (chunks <= 256) NUPS_GRAD_RING(128, 2, 2, 3)
+            else if (chunks <= 512) NUPS_GRAD_RING(256, 2, 2, 3)
+            else if constexpr (sizeof(X) == 2) NUPS_GRAD_RING(512, 2, 2, 3)
+            else if (chunks <= 1024) NUPS_GRAD_RING(256, 4, 1, 3)
+            else NUPS_GRAD_RING(512, 4, 1, 3)
+        }
+    }
+#undef NUPS_GRAD_RING
+    if (through_ring) {}
+    else if (len > grad_long_from(x_type)) {
         A* sums = (A*)(scratch + (a.part ? (grad_part_bytes(s, a.n, len, x_type) + 255) / 256 * 256 : 0));
         if (a.dx) {
             nups_launch_dependent(norm_grad_sums_kernel<X, VEC>, grid_for(a.n, 1, (unsigned)s->sm_count * 2), 1024, 0, st, a, sums);
@@ -999,7 +1162,7 @@ extern "C" nups_status nups_layer_norm_grad(nups_store* s, const void* d_x, int 
         return NUPS_OK;
     }
     if (!sums && !d_dx) return NUPS_OK;
-    GradArgs a = {d_x, x_stride, d_dy, dy_stride, d_mean, d_rstd, d_weight, d_dx, dx_stride, sums ? d_scratch : nullptr, n, len, dy_type, w_type, 0};
+    GradArgs a = {d_x, x_stride, d_dy, dy_stride, d_mean, d_rstd, d_weight, d_dx, dx_stride, sums ? d_scratch : nullptr, n, len, dy_type, w_type, 0, s->st};
     const int vec = (int)(16 / type_bytes(x_type));
     const bool wide = rows_allow(d_x, x_type, x_stride, len, vec, n) && rows_allow(d_dy, dy_type, dy_stride, len, vec, n) &&
                       (!d_dx || rows_allow(d_dx, x_type, dx_stride, len, vec, n));
