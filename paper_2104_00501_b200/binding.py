@@ -598,6 +598,34 @@ class Store:
             self._chk(rc, w)
         return out
 
+    def orthogonalize(self, update, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7, scale=1.0, out=None):
+        """`scale` times the Newton-Schulz iterate of a matrix [rows, cols] or of a batch of them [batch, rows, cols]; out may be
+        the update itself.  What push adds to rows that hold matrices: scale = -rate, out as [batch, rows * cols]."""
+        w = "nups_orthogonalize"
+        if out is None:
+            out = torch.empty_like(update, memory_format=torch.contiguous_format)
+        self._on_device(w, update, out)
+        if update.dim() not in (2, 3) or out.shape != update.shape or out.dtype != update.dtype or len(coefficients) != 3:
+            raise NupsError(EINVAL, w, "expected a matrix or a batch of them, out of the same shape and type, three coefficients")
+        (batch, rows, cols), places = (1,) * (3 - update.dim()) + tuple(update.shape), []
+        for t in (update, out):
+            if cols > 1 and t.stride(-1) != 1:
+                raise NupsError(EINVAL, w, "the values of a row must be contiguous")
+            places.append((t.data_ptr(), t.stride(-2) if rows > 1 else cols, t.stride(0) if batch > 1 and t.dim() == 3 else 0))
+            if places[-1][1] < 0 or places[-1][2] < 0:
+                raise NupsError(EINVAL, w, "strides must not be negative")
+        size = self._scratch_bytes("nups_orthogonalize_scratch", batch, rows, cols)
+        (pg, gs, gb), (po, os_, ob) = places
+        stream, kind = _stream(), _type(update)
+        scratch = _scratch_alloc(size, stream) if size else None
+        rc = self._l.nups_orthogonalize(self._s, pg, kind, gs, gb, batch, rows, cols, steps, (C.c_float * 3)(*coefficients), eps, scale, po, os_, ob,
+                                        scratch, size, stream)
+        if scratch:
+            _scratch_free(scratch)
+        if rc:
+            self._chk(rc, w)
+        return out
+
     # -- status -------------------------------------------------------------------------
     def status_check(self):
         return self._l.nups_status_check(self._s, _stream())

@@ -66,6 +66,20 @@ __device__ __forceinline__ float2 join2(uint32_t hi, uint32_t lo)
     const float2 a = __half22float2(*(const __half2*)&hi), b = __half22float2(*(const __half2*)&lo);
     return make_float2(a.x + b.x, a.y + b.y);
 }
+// Sum of the squares of N floats of any size: scaled by the power of two that brings the largest near 1, added in fp32, and only
+// the sum is widened (converting every value took 30 us for 4096 x 4096).  Scaling all of a matrix by a power of two changes no bit.
+template <int N> __device__ __forceinline__ double sum_of_squares(const float* v)
+{
+    float most = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) most = fmaxf(most, fabsf(v[i]));
+    const int e = max(254 - (int)(__float_as_uint(most) >> 23), 1);      // exponent field of the factor
+    const float f = __int_as_float(e << 23);
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum = fmaf(v[i] * f, v[i] * f, sum);
+    return (double)sum * __hiloint2double((1023 + 2 * (127 - e)) << 20, 0);
+}
 __device__ __forceinline__ double warp_sum_f64(double x)
 {
 #pragma unroll
@@ -73,10 +87,23 @@ __device__ __forceinline__ double warp_sum_f64(double x)
     return x;
 }
 
+// 32 results of each of a warp's 32 rows (one row per lane) to a row-major matrix, through shared memory so that a store covers
+// one row.  at: the first row's first value.
+__device__ __forceinline__ void write_rows(void* out, int type, uint64_t at, uint64_t stride, uint32_t rows, uint32_t cols, const float* v, float* tile)
+{
+    const uint32_t lane = threadIdx.x & 31;
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < 32; ++j) tile[lane * 33 + j] = v[j];
+    __syncwarp();
+    if (lane < cols)
+        for (uint32_t r = 0; r < min(rows, 32u); ++r) write_value(out, type, at + r * stride + lane, tile[r * 33 + lane]);
+}
+
 // ---------------------------------------------------------------------------------------------
 // one block per matrix
 // ---------------------------------------------------------------------------------------------
-constexpr int SMALL_M = 128, SMALL_N = 256, SMALL_BLOCK = 256;
+constexpr int SMALL_M = 128, SMALL_N = 256;
 constexpr uint32_t PANEL = 128 * 128;      // bytes of 64 columns of 128 rows: the unit of the operands' layout
 
 // Byte offset of column c of row r in an operand made of panels.
@@ -97,6 +124,9 @@ __device__ __forceinline__ uint32_t small_columns(uint32_t m16, uint32_t n16)
     return columns;
 }
 
+// Threads: 512 where a step's results take more than two warps per quarter of the rows (64 matrices of 100 x 100: 53 us with 256,
+// 41 with 512), 256 where they do not and several blocks fit a multiprocessor (600 of 64 x 64: 97 us with 256, 127 with 512).
+template <int TYPE, int SMALL_BLOCK>
 __global__ void __launch_bounds__(SMALL_BLOCK) orthogonalize_small_kernel(OrthArgs a)
 {
     extern __shared__ char raw[];
@@ -119,13 +149,27 @@ __global__ void __launch_bounds__(SMALL_BLOCK) orthogonalize_small_kernel(OrthAr
     if (warp == 0) tmem_alloc<1>(smem_address(&tmem_mem), columns);
     for (uint32_t i = threadIdx.x; i < (nb + mb) * 2 * PANEL / 16; i += SMALL_BLOCK) ((uint4*)base)[i] = make_uint4(0, 0, 0, 0);
     grid_dependency_wait();
-    const char* g = (const char*)a.g + (uint64_t)blockIdx.x * a.gb * (a.type == NUPS_F32 ? 4 : 2);
-    const uint32_t count = a.rows * a.cols;
+    const char* g = (const char*)a.g + (uint64_t)blockIdx.x * a.gb * (TYPE == NUPS_F32 ? 4 : 2);
+    // a warp per row, four rows' loads in flight: v[k][j] is column 2 lane + 64 k + j, zero beyond the row; row(r, v)
+    auto each_row = [&](auto row) {
+        for (uint32_t r0 = warp; r0 < a.rows; r0 += 4 * (SMALL_BLOCK / 32)) {
+            float v[4][SMALL_N / 64][2];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int k = 0; k < SMALL_N / 64; ++k)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const uint32_t r = r0 + u * (SMALL_BLOCK / 32), c = 2 * lane + 64 * k + j;
+                        v[u][k][j] = r < a.rows && c < a.cols ? read_value(g, TYPE, (uint64_t)r * a.gs + c) : 0.0f;
+                    }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (r0 + u * (SMALL_BLOCK / 32) < a.rows) row(r0 + u * (SMALL_BLOCK / 32), v[u]);
+        }
+    };
     double sum = 0;
-    for (uint32_t i = threadIdx.x; i < count; i += SMALL_BLOCK) {
-        const float x = read_value(g, a.type, (uint64_t)(i / a.cols) * a.gs + i % a.cols);
-        sum += (double)x * x;
-    }
+    each_row([&](uint32_t, const float (&v)[SMALL_N / 64][2]) { sum += sum_of_squares<SMALL_N / 32>(&v[0][0]); });
     sum = warp_sum_f64(sum);
     if (lane == 0) sums[warp] = sum;
     tc_fence_before();
@@ -136,14 +180,30 @@ __global__ void __launch_bounds__(SMALL_BLOCK) orthogonalize_small_kernel(OrthAr
 #pragma unroll
     for (int w = 0; w < SMALL_BLOCK / 32; ++w) sum += sums[w];
     const float inv = (float)((double)X_SCALE / (sqrt(sum) + (double)a.eps));
-    for (uint32_t i = threadIdx.x; i < count; i += SMALL_BLOCK) {
-        const uint32_t r = i / a.cols, c = i % a.cols;
-        __half hi, lo;
-        split(read_value(g, a.type, (uint64_t)r * a.gs + c) * inv, hi, lo);
-        const uint32_t at = a.tall ? panel_at(c, r) : panel_at(r, c);
-        *(__half*)(x_hi + at) = hi;
-        *(__half*)(x_lo + at) = lo;
-    }
+    each_row([&](uint32_t r, const float (&v)[SMALL_N / 64][2]) {
+#pragma unroll
+        for (int k = 0; k < SMALL_N / 64; ++k) {
+            const uint32_t c = 2 * lane + 64 * k;
+            if (c >= a.cols) continue;                      // what is beyond the matrix is zero, as it was
+            const float x = v[k][0] * inv, y = v[k][1] * inv;
+            const __half2 hi = __floats2half2_rn(x, y);
+            const float2 f = __half22float2(hi);
+            const __half2 lo = __floats2half2_rn(x - f.x, y - f.y);
+            if (!a.tall) {
+                const uint32_t at = panel_at(r, c);
+                *(__half2*)(x_hi + at) = hi;
+                *(__half2*)(x_lo + at) = lo;
+            } else {
+                const uint32_t at = panel_at(c, r), next = panel_at(c + 1, r);
+                *(__half*)(x_hi + at) = __low2half(hi);
+                *(__half*)(x_lo + at) = __low2half(lo);
+                if (c + 1 < a.cols) {
+                    *(__half*)(x_hi + next) = __high2half(hi);
+                    *(__half*)(x_lo + next) = __high2half(lo);
+                }
+            }
+        }
+    });
     const uint32_t quarter = (warp & 3) * 32, row = quarter + lane;       // tensor-memory lanes that this warp may read
     const uint32_t sxh = smem_address(x_hi), sxl = smem_address(x_lo), sah = smem_address(a_hi), sal = smem_address(a_lo);
     uint32_t phase = 0;
@@ -165,7 +225,7 @@ __global__ void __launch_bounds__(SMALL_BLOCK) orthogonalize_small_kernel(OrthAr
             }
             tc_commit<1>(bar);
         }
-        const bool ok = mbar_wait(bar, phase & 1);
+        const bool ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar, phase & 1));
         ++phase;
         tc_fence_after();
         return ok;
@@ -198,7 +258,7 @@ __global__ void __launch_bounds__(SMALL_BLOCK) orthogonalize_small_kernel(OrthAr
     for (uint32_t step = 0; step < a.steps; ++step) {
         // A = X X^T
         bool ok = issue(sxh, sxl, sxh, sxl, false, m16, n16 / 16);
-        for (uint32_t c0 = (warp >> 2) * 32; c0 < m16; c0 += 64) {
+        for (uint32_t c0 = (warp >> 2) * 32; c0 < m16; c0 += SMALL_BLOCK / 4) {
             float v[32];
             sum_runs(c0, m16, n16 / 16, v);
 #pragma unroll
@@ -210,7 +270,7 @@ __global__ void __launch_bounds__(SMALL_BLOCK) orthogonalize_small_kernel(OrthAr
         if (__syncthreads_or(!ok)) { dead = true; break; }
         // B = a I + b A + c A^2, in A's place once the products have read it
         ok = issue(sah, sal, sah, sal, false, m16, m16 / 16);
-        for (uint32_t c0 = (warp >> 2) * 32; c0 < m16; c0 += 64) {
+        for (uint32_t c0 = (warp >> 2) * 32; c0 < m16; c0 += SMALL_BLOCK / 4) {
             float v[32];
             sum_runs(c0, m16, m16 / 16, v);
 #pragma unroll
@@ -236,18 +296,21 @@ __global__ void __launch_bounds__(SMALL_BLOCK) orthogonalize_small_kernel(OrthAr
         // X = B X
         ok = issue(sah, sal, sxh, sxl, true, n16, m16 / 16);
         const bool last = step + 1 == a.steps;
-        char* out = (char*)a.out + (uint64_t)blockIdx.x * a.ob * (a.type == NUPS_F32 ? 4 : 2);
-        for (uint32_t c0 = (warp >> 2) * 32; c0 < n16; c0 += 64) {
+        char* out = (char*)a.out + (uint64_t)blockIdx.x * a.ob * (TYPE == NUPS_F32 ? 4 : 2);
+        for (uint32_t c0 = (warp >> 2) * 32; c0 < n16; c0 += SMALL_BLOCK / 4) {
             float v[32];
             sum_runs(c0, n16, m16 / 16, v);
             if (last) {
-                if (ok && row < a.m)
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[j] *= FROM_BX * a.scale;
+                if (!ok || quarter >= a.m || c0 >= a.n) continue;          // ok: the same for all threads but after a second's wait in vain
+                if (!a.tall) {
+                    write_rows(out, TYPE, (uint64_t)quarter * a.os + c0, a.os, a.m - quarter, a.n - c0, v, (float*)base + warp * 32 * 33);
+                } else if (row < a.m) {
 #pragma unroll
                     for (int j = 0; j < 32; ++j)
-                        if (c0 + j < a.n) {
-                            const float x = v[j] * FROM_BX * a.scale;
-                            write_value(out, a.type, a.tall ? (uint64_t)(c0 + j) * a.os + row : (uint64_t)row * a.os + c0 + j, x);
-                        }
+                        if (c0 + j < a.n) write_value(out, TYPE, (uint64_t)(c0 + j) * a.os + row, v[j]);
+                }
             } else {
 #pragma unroll
                 for (int j = 0; j < 32; ++j) v[j] *= FROM_BX * X_SCALE;
@@ -305,8 +368,7 @@ __global__ void __launch_bounds__(256) orth_squares_kernel(OrthArgs a, double* s
 #pragma unroll
             for (int k = 0; k < 4; ++k) x[4 * u + k] = i < runs && c + 256 * k < a.cols ? read_value(g, a.type, (uint64_t)r * a.gs + c + 256 * k) : 0.0f;
         }
-#pragma unroll
-        for (int k = 0; k < 16; ++k) sum += (double)x[k] * x[k];
+        sum += sum_of_squares<16>(x);
     }
     sum = warp_sum_f64(sum);
     if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = sum;
@@ -386,19 +448,6 @@ template <int THREADS> __device__ __forceinline__ bool group_all(uint32_t group,
 
 // How many tiles of the 256 rows bi of a symmetric result reach the diagonal or lie below it.
 __host__ __device__ constexpr uint32_t tiles_of_rows(uint32_t bi, uint32_t tile_n) { return (PAIR_M / tile_n) * (bi + 1); }
-
-// 32 results of each of a warp's 32 rows (one row per lane) to a row-major matrix, through shared memory so that a store covers
-// one row.  at: the first row's first value.
-__device__ __forceinline__ void write_rows(void* out, int type, uint64_t at, uint64_t stride, uint32_t rows, uint32_t cols, const float* v, float* tile)
-{
-    const uint32_t lane = threadIdx.x & 31;
-    __syncwarp();
-#pragma unroll
-    for (int j = 0; j < 32; ++j) tile[lane * 33 + j] = v[j];
-    __syncwarp();
-    if (lane < cols)
-        for (uint32_t r = 0; r < min(rows, 32u); ++r) write_value(out, type, at + r * stride + lane, tile[r * 33 + lane]);
-}
 
 // A tile of 256 x TILE_N results (128 or 256) by a pair of blocks, 128 rows each.  In each block warp 0 brings in the operands' pairs by TMA; warp 1
 // of the first block issues the products of both (cta_group::2: each block reads its own rows of A and half of B, so shared
@@ -777,10 +826,25 @@ nups_status launch_tiled(nups_store* s, const Maps& a, const Maps& b, const Maps
 
 // Large dynamic shared memory, asked for once on the store's device.
 template <int MODE, int TILE_N> cudaError_t opt_in_tiled() { return cudaFuncSetAttribute(orth_tiled_kernel<MODE, TILE_N>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TILED_SMEM); }
+template <int TYPE> cudaError_t opt_in_small()
+{
+    const int most = (int)small_smem(SMALL_M, SMALL_N);
+    const cudaError_t e = cudaFuncSetAttribute(orthogonalize_small_kernel<TYPE, 256>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+    return e != cudaSuccess ? e : cudaFuncSetAttribute(orthogonalize_small_kernel<TYPE, 512>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+}
+template <int TYPE> nups_status launch_small(nups_store* s, const OrthArgs& o, uint32_t batch, cudaStream_t st)
+{
+    const unsigned block = o.n > 64 ? 512 : 256;            // o.m <= o.n
+    CK(nups_launch_dependent(block == 512 ? orthogonalize_small_kernel<TYPE, 512> : orthogonalize_small_kernel<TYPE, 256>, dim3(batch), block, small_smem(o.m, o.n), st, o));
+    LAUNCH_CHECK(s);
+    return NUPS_OK;
+}
 nups_status opt_in(nups_store* s)
 {
     if (s->orth_smem_opted) return NUPS_OK;
-    CK(cudaFuncSetAttribute(orthogonalize_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)small_smem(SMALL_M, SMALL_N)));
+    CK(opt_in_small<NUPS_F32>());
+    CK(opt_in_small<NUPS_F16>());
+    CK(opt_in_small<NUPS_BF16>());
     CK((opt_in_tiled<GRAM, 128>()));
     CK((opt_in_tiled<GRAM, 256>()));
     CK((opt_in_tiled<POLYNOMIAL, 128>()));
@@ -878,11 +942,7 @@ extern "C" nups_status nups_orthogonalize(nups_store* s, const void* d_update, i
                         h_coefficients[0], h_coefficients[1], h_coefficients[2], eps, scale, s->st};
     rc = opt_in(s);
     if (rc != NUPS_OK) return rc;
-    if (small_form(o.m, o.n)) {
-        const uint32_t smem = small_smem(o.m, o.n);
-        CK(nups_launch_dependent(orthogonalize_small_kernel, dim3(batch), SMALL_BLOCK, smem, st, o));
-        LAUNCH_CHECK(s);
-        return NUPS_OK;
-    }
+    if (small_form(o.m, o.n))
+        return type == NUPS_F32 ? launch_small<NUPS_F32>(s, o, batch, st) : type == NUPS_F16 ? launch_small<NUPS_F16>(s, o, batch, st) : launch_small<NUPS_BF16>(s, o, batch, st);
     return launch_large(s, o, batch, (char*)d_scratch, st);
 }
