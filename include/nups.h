@@ -362,7 +362,9 @@ nups_status nups_get_clip_stats(nups_store* store, double* h_sum, uint64_t* h_co
  *   - x_type and the like are NUPS_F32, NUPS_F64, NUPS_F16 or NUPS_BF16.
  *   - Row i of a matrix argument starts `stride` VALUES after row i - 1 and its
  *     values are contiguous; rows of an output must not overlap.  Any alignment
- *     that suits the type is allowed, 16-byte aligned rows are fastest.
+ *     that suits the type is allowed, 16-byte aligned rows are fastest.  An output
+ *     overlaps an input only where a call names it (the same rows in the same
+ *     places), and no other output.
  *   - Sums and statistics are held in fp32, or fp64 for fp64 values.
  *   - d_scratch is the caller's device memory, 256-byte aligned, of at least the
  *     bytes that the *_scratch call names for the same sizes; it needs no
