@@ -1041,7 +1041,7 @@ unsigned grad_blocks(const nups_store* s, uint64_t n, uint32_t len, int type)
     const unsigned sm = (unsigned)s->sm_count;
     const uint32_t bytes = len * (uint32_t)type_bytes(type);
     if (len > grad_long_from(type)) return grid_for(n, 16, 32);
-    return grid_for(n, bytes <= 128 ? 64 : bytes <= 1024 ? 8 : 2, sm * (bytes <= 1024 ? 3 : bytes <= 4096 ? 4 : bytes <= 8192 ? 2 : 1));
+    return grid_for(n, bytes <= 128 ? 64 : bytes <= 1024 ? 8 : 2, sm * (bytes <= 1024 ? 3 : bytes <= 4096 ? 4 : bytes <= (type_bytes(type) == 2 ? 8192u : 16384u) ? 2 : 1));
 }
 uint64_t grad_part_bytes(const nups_store* s, uint64_t n, uint32_t len, int type)
 {

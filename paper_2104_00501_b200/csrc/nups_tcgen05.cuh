@@ -64,7 +64,6 @@ __device__ __forceinline__ void tma_store(const void* map, int x, int y, int z, 
 }
 __device__ __forceinline__ void tma_store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void tma_store_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }   // shared memory may be reused
-__device__ __forceinline__ void tma_store_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
 // Tensor memory: 32-bit columns of 128 lanes, allocated and freed by one whole warp.
 // (P = 2: a warp of each block of the pair).

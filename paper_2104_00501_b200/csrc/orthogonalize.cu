@@ -675,7 +675,7 @@ orth_tiled_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 tma_store(&map_to, (int)panel_col, (int)row0, z + 1, smem_address(panel + PANEL));
                 tma_store_commit();
             }
-            if (first) tma_store_wait();
+            if (first) tma_store_wait_read();               // the writes are done when the grid is
         }
     }
     if (!ok) atomicCAS(&o.st->status, 0, NUPS_ETIMEOUT);
