@@ -62,7 +62,11 @@ def test_normalised_pull():
     rows = s.pull(at)
     y, mean, rstd, pulled = s.pull_norm(at, rows=True)
     assert torch.equal(pulled, rows) and s.status_check() == binding.EKEY
-    assert torch.allclose(y, torch.nn.functional.layer_norm(rows, (length,)), atol=1e-5)
+    x = rows.double()
+    d = x - x.mean(1, keepdim=True)
+    ref = d / torch.sqrt((d * d).mean(1, keepdim=True) + 1e-5)
+    # 64 roundings of 2^-24, as for layer norm elsewhere; the mean of the magnitudes over the deviation is below 1 here
+    assert ((y.double() - ref).abs() <= 64 * 2.0 ** -24 * (ref.abs() + 1)).all()
     s.close()
 
 
