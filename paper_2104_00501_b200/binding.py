@@ -175,6 +175,7 @@ def _type(t) -> int:
 
 # Scratch of one call from torch's allocator, on the call's stream and (while one is captured) in its graph's pool: given back as
 # soon as the call's work is enqueued, later work of the stream may have it.  A fourth of the host time of a tensor.
+_current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 _scratch_alloc, _scratch_free = torch._C._cuda_cudaCachingAllocator_raw_alloc, torch._C._cuda_cudaCachingAllocator_raw_delete
 
 
@@ -402,10 +403,10 @@ class Store:
     # bound by the host, so the checks are written for the case that passes.
     def _on_device(self, what, *tensors):
         here = self._index
-        if torch._C._cuda_getDevice() != here:
+        if _current_device() != here:
             raise NupsError(ESTATE, what, f"the store is on {self.device}, which is not the current device")
         for t in tensors:
-            if t is not None and (not t.is_cuda or t.get_device() != here):
+            if t is not None and t.get_device() != here:    # -1: host memory
                 raise NupsError(EINVAL, what, f"a tensor is on {t.device}, the store on {self.device}")
 
     def _scratch_bytes(self, fn, *sizes):
@@ -425,6 +426,8 @@ class Store:
         shape = t.shape
         if len(shape) != 2 or (n is not None and (shape[0] != n or shape[1] != length)):
             raise NupsError(EINVAL, what, f"expected a matrix{'' if n is None else f' of {n} x {length}'}, got {tuple(shape)}")
+        if t.is_contiguous():
+            return t.data_ptr(), shape[1]
         stride, step = t.stride()
         if step != 1 and shape[1] > 1:
             raise NupsError(EINVAL, what, "the values of a row must be contiguous")
@@ -437,21 +440,21 @@ class Store:
     def _vector(self, what, t, length, dtype=None):
         if t is None:
             return None
-        if t.dim() != 1 or t.shape[0] != length or (length > 1 and t.stride(0) != 1) or (dtype is not None and t.dtype != dtype):
+        if t.shape != (length,) or not t.is_contiguous() or (dtype is not None and t.dtype != dtype):
             raise NupsError(EINVAL, what, f"expected {length} contiguous values{'' if dtype is None else f' of {dtype}'}, got {tuple(t.shape)} of {t.dtype}")
         return t.data_ptr()
 
-    def _params(self, what, x_dtype, length, *vectors):
+    def _params(self, what, x_dtype, length, weight, bias=None):
         """Type of the parameters given (x's type, or float32), and their addresses."""
-        dtype, at = None, []
-        for v in vectors:
-            if v is not None:
-                if dtype is None:
-                    dtype = v.dtype
-                elif v.dtype != dtype:
-                    raise NupsError(EINVAL, what, "weight and bias must be of one type")
-            at.append(self._vector(what, v, length))
-        return x_dtype if dtype is None else dtype, at
+        if weight is None:
+            return (x_dtype, None, None) if bias is None else (bias.dtype, None, self._vector(what, bias, length))
+        dtype = weight.dtype
+        return dtype, self._vector(what, weight, length), None if bias is None else self._bias(what, bias, length, dtype)
+
+    def _bias(self, what, bias, length, dtype):
+        if bias.dtype != dtype:
+            raise NupsError(EINVAL, what, "weight and bias must be of one type")
+        return self._vector(what, bias, length)
 
     def layer_norm(self, x, weight=None, bias=None, eps=1e-5, out_dtype=None, stats=True, out=None):
         """(y, mean, rstd) of the rows of x [n, len]; stats=False: y alone.  out may be x itself."""
@@ -462,7 +465,7 @@ class Store:
         px, xs = self._rows(w, x)
         n, length = x.shape
         py, ys = self._rows(w, out, n, length)
-        dtype, (pw, pb) = self._params(w, x.dtype, length, weight, bias)
+        dtype, pw, pb = self._params(w, x.dtype, length, weight, bias)
         if stats:
             keep = torch.float64 if x.dtype == torch.float64 else torch.float32
             mean = torch.empty(n, dtype=keep, device=self.device)
@@ -470,7 +473,7 @@ class Store:
             pm, pr = mean.data_ptr(), rstd.data_ptr()
         else:
             pm = pr = None
-        rc = self._l.nups_layer_norm(self._s, px, _type(x), xs, n, length, pw, pb, TYPES.get(dtype, -1), eps, py, _type(out), ys, pm, pr, _stream())
+        rc = self._l.nups_layer_norm(self._s, px, _type(x), xs, n, length, pw, pb, TYPES.get(dtype, -1), eps, py, _type(out), ys, pm, pr, _current_stream(self._index))
         if rc:
             self._chk(rc, w)
         return (out, mean, rstd) if stats else out
@@ -479,7 +482,7 @@ class Store:
         """Layer norm of the pulled rows: (y, mean, rstd), and with rows=True also the rows; stats=False: without mean and rstd."""
         w, n, mine = "nups_pull_norm", keys.numel(), self.dtype
         self._on_device(w, keys, weight, bias)
-        dtype, (pw, pb) = self._params(w, mine, self.L, weight, bias)
+        dtype, pw, pb = self._params(w, mine, self.L, weight, bias)
         if dtype != mine:
             raise NupsError(EINVAL, w, f"weight and bias must be of the store's type, {mine}")
         pk = _ptr(keys, torch.int32)
@@ -493,7 +496,7 @@ class Store:
             mean = torch.empty(n, dtype=mine, device=self.device)
             rstd = torch.empty(n, dtype=mine, device=self.device)
             pm, pr = mean.data_ptr(), rstd.data_ptr()
-        rc = self._l.nups_pull_norm(self._s, pk, n, pw, pb, eps, y.data_ptr(), _type(y), pp, pm, pr, _stream())
+        rc = self._l.nups_pull_norm(self._s, pk, n, pw, pb, eps, y.data_ptr(), _type(y), pp, pm, pr, _current_stream(self._index))
         if rc:
             self._chk(rc, w)
         if stats:
@@ -516,8 +519,8 @@ class Store:
                 raise NupsError(EINVAL, w, "dx must have x's type")
         keep = torch.float64 if x.dtype == torch.float64 else torch.float32
         pm, pr = self._vector(w, mean, n, keep), self._vector(w, rstd, n, keep)
-        dtype, (pw,) = self._params(w, x.dtype, length, weight)
-        x_type, stream = _type(x), _stream()
+        dtype, pw, _ = self._params(w, x.dtype, length, weight)
+        x_type, stream = _type(x), _current_stream(self._index)
         dweight = dbias = pdw = pdb = None
         if need_params:
             dweight = torch.empty(length, dtype=dtype, device=self.device)
@@ -558,7 +561,7 @@ class Store:
         if losses or (losses is None and (balance != 0.0 or z != 0.0)):
             prob, loss, lse = (torch.empty(k, dtype=torch.float32, device=dev) for k in (experts, 3, n))
             pp, pl, pe = prob.data_ptr(), loss.data_ptr(), lse.data_ptr()
-        size, stream = self._scratch_bytes("nups_route_scratch", n, experts), _stream()
+        size, stream = self._scratch_bytes("nups_route_scratch", n, experts), _current_stream(self._index)
         scratch = _scratch_alloc(size, stream) if size else None
         rc = self._l.nups_route(self._s, p, kind, stride, n, experts, top, pa, renormalize, balance, z, choice.data_ptr(), weight.data_ptr(), pe,
                                 counts.data_ptr(), tokens.data_ptr(), pp, pl, scratch, size, stream)
@@ -593,7 +596,7 @@ class Store:
             raise NupsError(EINVAL, w, "dloss must be one float32")
         rc = self._l.nups_route_grad(self._s, p, _type(logits), stride, n, experts, top, self._active(w, r.active, n), r.renormalize, r.balance, r.z,
                                      r.choice.data_ptr(), r.weight.data_ptr(), r.lse.data_ptr(), r.counts.data_ptr(), r.tokens.data_ptr(),
-                                     None if dloss is None else dloss.data_ptr(), pdw, po, os_, _stream())
+                                     None if dloss is None else dloss.data_ptr(), pdw, po, os_, _current_stream(self._index))
         if rc:
             self._chk(rc, w)
         return out
@@ -616,7 +619,7 @@ class Store:
                 raise NupsError(EINVAL, w, "strides must not be negative")
         size = self._scratch_bytes("nups_orthogonalize_scratch", batch, rows, cols)
         (pg, gs, gb), (po, os_, ob) = places
-        stream, kind = _stream(), _type(update)
+        stream, kind = _current_stream(self._index), _type(update)
         scratch = _scratch_alloc(size, stream) if size else None
         rc = self._l.nups_orthogonalize(self._s, pg, kind, gs, gb, batch, rows, cols, steps, (C.c_float * 3)(*coefficients), eps, scale, po, os_, ob,
                                         scratch, size, stream)
