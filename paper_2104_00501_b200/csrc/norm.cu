@@ -522,16 +522,9 @@ nups_status launch_norm(nups_store* s, const NormArgs& a, const View& v, cudaStr
         // 8 lanes of 4 chunks, 209 with 16 of 2, two rows each, 278 with 32 of 1, four rows each)
         if (chunks <= 4) NUPS_NORM(4, 1, 2)
         else if (chunks <= 8) NUPS_NORM(4, 2, 1)
-        else if constexpr (VEC <= 4) {
-            if (chunks <= 16) NUPS_NORM(4, 4, 1)
-            else if (chunks <= 32) NUPS_NORM(8, 4, 1)
-            else if (chunks <= 64) NUPS_NORM(16, 4, 1)
-        } else {
-            if (chunks <= 16) NUPS_NORM(8, 2, 1)
-            else if (chunks <= 32) NUPS_NORM(16, 2, 1)
-            else if (chunks <= 64) NUPS_NORM(32, 2, 1)
-        }
-        if (chunks <= 64) {}
+        else if (chunks <= 16) NUPS_NORM((VEC <= 4 ? 4 : 8), (VEC <= 4 ? 4 : 2), 1)
+        else if (chunks <= 32) NUPS_NORM((VEC <= 4 ? 8 : 16), (VEC <= 4 ? 4 : 2), 1)
+        else if (chunks <= 64) NUPS_NORM((VEC <= 4 ? 16 : 32), (VEC <= 4 ? 4 : 2), 1)
         else if (chunks <= 128) NUPS_NORM(128, 1, 4)
         else if (chunks <= 256) NUPS_NORM(128, 2, 4)
         else if (chunks <= 512) NUPS_NORM(256, 2, 4)
@@ -1084,8 +1077,9 @@ nups_status launch_grad(nups_store* s, GradArgs a, int x_type, void* d_dw, void*
         }
     }
 #undef NUPS_GRAD_RING
-    if (through_ring) {}
-    else if (len > grad_long_from(x_type)) {
+    if (through_ring) {
+        // launched above
+    } else if (len > grad_long_from(x_type)) {
         A* sums = (A*)(scratch + (a.part ? (grad_part_bytes(s, a.n, len, x_type) + 255) / 256 * 256 : 0));
         if (a.dx) {
             nups_launch_dependent(norm_grad_sums_kernel<X, VEC>, grid_for(a.n, 1, (unsigned)s->sm_count * 2), 1024, 0, st, a, sums);
@@ -1121,8 +1115,12 @@ nups_status launch_grad(nups_store* s, GradArgs a, int x_type, void* d_dw, void*
     LAUNCH_CHECK(s);
     if (a.part) {
         const dim3 grid((len + 31) / 32, 2);
-        if (sizeof(X) == 2 && a.w_type == NUPS_F32) nups_launch_dependent(norm_grad_join_kernel<A, float>, grid, 1024, 0, st, (const A*)a.part, blocks, len, (float*)d_dw, (float*)d_db);
-        else nups_launch_dependent(norm_grad_join_kernel<A, X>, grid, 1024, 0, st, (const A*)a.part, blocks, len, (X*)d_dw, (X*)d_db);
+        bool wide_params = false;                           // fp32 parameters of 16-bit rows
+        if constexpr (sizeof(X) == 2) {
+            wide_params = a.w_type == NUPS_F32;
+            if (wide_params) nups_launch_dependent(norm_grad_join_kernel<A, float>, grid, 1024, 0, st, (const A*)a.part, blocks, len, (float*)d_dw, (float*)d_db);
+        }
+        if (!wide_params) nups_launch_dependent(norm_grad_join_kernel<A, X>, grid, 1024, 0, st, (const A*)a.part, blocks, len, (X*)d_dw, (X*)d_db);
         LAUNCH_CHECK(s);
     }
     return NUPS_OK;

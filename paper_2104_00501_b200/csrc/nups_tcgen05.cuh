@@ -87,13 +87,11 @@ __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::
 // Shared memory written by ordinary stores is visible to later products and bulk copies.
 __device__ __forceinline__ void async_proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-// Operand in shared memory.  K-major: rows of `row_bytes` (128: 64 values of K, 64: 32 values) with the matching swizzle, groups of
-// eight rows one after the other.  MN-major: 128-byte runs of 64 values along M or N, one run per value of K, the next 64
+// Operand in shared memory, 128-byte swizzle.  K-major: rows of 64 values of K, groups of eight rows one after the other.  MN-major: 128-byte runs of 64 values along M or N, one run per value of K, the next 64
 // values along M or N `next_block` bytes further.
-__device__ __forceinline__ uint64_t operand_k_major(uint32_t address, int row_bytes)
+__device__ __forceinline__ uint64_t operand_k_major(uint32_t address)
 {
-    const uint64_t layout = row_bytes == 128 ? 2 : 4;      // 128-byte and 64-byte swizzle
-    return (uint64_t)((address & 0x3FFFF) >> 4) | (1ull << 16) | ((uint64_t)(8 * row_bytes >> 4) << 32) | (1ull << 46) | (layout << 61);
+    return (uint64_t)((address & 0x3FFFF) >> 4) | (1ull << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
 __device__ __forceinline__ uint64_t operand_mn_major(uint32_t address, uint32_t next_block)
 {
@@ -135,12 +133,3 @@ __device__ __forceinline__ void tmem_load32(uint32_t address, float (&v)[32])
         : "r"(address));
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
-// 16 columns likewise; the values are there after tmem_load_wait().
-__device__ __forceinline__ void tmem_load16(uint32_t address, float* v)
-{
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]),
-                   "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
-                 : "r"(address));
-}
-__device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }

@@ -28,7 +28,6 @@ template <class A> __device__ __forceinline__ A widen(__nv_bfloat16 x) { return 
 template <class T, class A> struct Narrow;
 template <> struct Narrow<float, float> { static __device__ __forceinline__ float of(float x) { return x; } };
 template <> struct Narrow<double, double> { static __device__ __forceinline__ double of(double x) { return x; } };
-template <> struct Narrow<float, double> { static __device__ __forceinline__ float of(double x) { return (float)x; } };
 template <> struct Narrow<__half, float> { static __device__ __forceinline__ __half of(float x) { return __float2half_rn(x); } };
 template <> struct Narrow<__nv_bfloat16, float> { static __device__ __forceinline__ __nv_bfloat16 of(float x) { return __float2bfloat16_rn(x); } };
 template <class T, class A> __device__ __forceinline__ T narrow(A x) { return Narrow<T, A>::of(x); }
