@@ -196,7 +196,20 @@ __global__ void __launch_bounds__(team_block(TPR)) norm_kernel(NormArgs a, View 
         load_params<X, A, VEC, TPR, CH>(a.b, a.w_type, a.w_vec, a.len, t, (A)0, b);
     }
     int turn = 0;
-    for (uint64_t base = (uint64_t)blockIdx.x * (TEAMS * ROWS); base < a.n; base += (uint64_t)gridDim.x * (TEAMS * ROWS), ++turn) {
+    // pull_norm: the lookups run ahead of the rows, the key two turns, the word that tells whether it is replicated one
+    const uint64_t step = (uint64_t)gridDim.x * (TEAMS * ROWS);
+    uint32_t key_a[ROWS], key_b[ROWS], bits_a[ROWS];
+    auto key_of = [&](uint64_t row) { return row < a.n ? __ldg(a.keys + row) : 0u; };
+    auto bits_of = [&](uint32_t key) { return v.H != 0 && key < v.num_keys ? __ldg(v.hot_bits + (key >> 5)) : 0u; };
+    if constexpr (KEYED)
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) {
+            const uint64_t row = (uint64_t)blockIdx.x * (TEAMS * ROWS) + k * TEAMS + team;
+            key_a[k] = key_of(row);
+            key_b[k] = key_of(row + step);
+            bits_a[k] = bits_of(key_a[k]);
+        }
+    for (uint64_t base = (uint64_t)blockIdx.x * (TEAMS * ROWS); base < a.n; base += step, ++turn) {
         Pack<X, VEC> x[ROWS][CH];
         const X* src[ROWS];
         const X* pend[ROWS];
@@ -204,12 +217,15 @@ __global__ void __launch_bounds__(team_block(TPR)) norm_kernel(NormArgs a, View 
         for (int k = 0; k < ROWS; ++k) {
             const uint64_t row = base + k * TEAMS + team;
             src[k] = pend[k] = nullptr;
-            if (row < a.n) {
-                if (KEYED) {
-                    const uint32_t key = __ldg(a.keys + row);
+            if constexpr (KEYED) {
+                const uint32_t key = key_a[k], bits = bits_a[k];
+                key_a[k] = key_b[k];
+                bits_a[k] = bits_of(key_a[k]);
+                key_b[k] = key_of(row + 2 * step);
+                if (row < a.n) {
                     if (key < v.num_keys) {
                         src[k] = (const X*)v.val + (uint64_t)key * a.len;
-                        if (key_is_hot(v, key)) {
+                        if ((bits >> (key & 31)) & 1u) {
                             const uint32_t slot = (uint32_t)__ldg(v.slot_of + key);
                             pend[k] = (const X*)v.dval + ((uint64_t)worker_of_item(row, a.n, v.R) * v.Hcap + slot) * a.len;
                         }
@@ -220,9 +236,9 @@ __global__ void __launch_bounds__(team_block(TPR)) norm_kernel(NormArgs a, View 
                     } else if (t == 0) {
                         flag_bad_key(v);
                     }
-                } else {
-                    src[k] = (const X*)a.x + row * a.xs;
                 }
+            } else if (row < a.n) {
+                src[k] = (const X*)a.x + row * a.xs;
             }
         }
 #pragma unroll
