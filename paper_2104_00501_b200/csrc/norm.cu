@@ -515,7 +515,7 @@ nups_status launch_norm(nups_store* s, const NormArgs& a, const View& v, cudaStr
         LAUNCH_CHECK(s);                                                                                                                   \
         return NUPS_OK;                                                                                                                    \
     }
-    if constexpr (VEC > 1 && !KEYED) {
+    if constexpr (VEC * sizeof(X) == 16 && !KEYED) {
         if (chunks > 64 && a.n > (uint64_t)s->sm_count) {   // fewer rows: every block has one group, nothing to run ahead of
             if (chunks <= 128) NUPS_RING(128, 1, 4, 3)
             if (chunks <= 256) NUPS_RING(128, 2, 4, 3)
@@ -533,7 +533,7 @@ nups_status launch_norm(nups_store* s, const NormArgs& a, const View& v, cudaStr
         const unsigned grid = grid_for(a.n, PER_BLOCK, (unsigned)s->sm_count * resident);                                                  \
         nups_launch_dependent(norm_kernel<X, VEC, TPR_, CH_, ROWS_, KEYED>, grid, team_block(TPR_), 0, st, a, v);                          \
     }
-    if constexpr (VEC > 1) {
+    if constexpr (VEC * sizeof(X) == 16) {
         // short rows: several teams to a warp with a few chunks per lane, one row each (1M pulled rows of 128 floats: 205 us with
         // 8 lanes of 4 chunks, 209 with 16 of 2, two rows each, 278 with 32 of 1, four rows each)
         if (chunks <= 4) NUPS_NORM(4, 1, 2)
@@ -549,10 +549,14 @@ nups_status launch_norm(nups_store* s, const NormArgs& a, const View& v, cudaStr
         else if (chunks <= 4096) NUPS_NORM(1024, 4, 1)
         else nups_launch_dependent(norm_long_kernel<X, VEC, KEYED>, grid_for(a.n, 1, (unsigned)s->sm_count * 2), 1024, 0, st, a, v);
     } else {
-        if (chunks <= 32) NUPS_NORM(32, 1, 4)
-        else if (chunks <= 64) NUPS_NORM(32, 2, 4)
-        else if (chunks <= 128) NUPS_NORM(32, 4, 4)
-        else if (chunks <= 256) NUPS_NORM(32, 8, 2)
+        // rows that 16-byte loads cannot read: pairs of 16-bit values where length and addresses are even, else single values.
+        // Forward with one or two rows of a few chunks per lane: 600,000 rows of 17 floats 32 us (85 with a warp and four rows),
+        // 400,000 rows of 34 bf16 24 us (63 by single values), 20,000 rows of 2046 bf16 41 us (55 by single values).
+        if (chunks <= 16) NUPS_NORM(4, 4, 1)
+        else if (chunks <= 32) NUPS_NORM(8, 4, 1)
+        else if (chunks <= 64) NUPS_NORM(16, 4, 1)
+        else if (chunks <= 128) NUPS_NORM(32, 4, 2)
+        else if (chunks <= 256) NUPS_NORM(32, 8, (VEC == 1 && sizeof(X) == 2 ? 2 : 1))
         else if (chunks <= 512) NUPS_NORM(32, 16, 1)
         else if (chunks <= 1024) NUPS_NORM(128, 8, 2)
         else if (chunks <= 2048) NUPS_NORM(256, 8, 2)
@@ -604,12 +608,13 @@ extern "C" nups_status nups_layer_norm(nups_store* s, const void* d_x, int x_typ
     cudaStream_t st = (cudaStream_t)stream;
     const int vec = (int)(16 / type_bytes(x_type));
     const bool wide = rows_allow(d_x, x_type, x_stride, len, vec, n) && rows_allow(d_y, y_type, y_stride, len, vec, n);
-    a.w_vec = wide && params_vec(a, x_type, vec);
+    const bool pairs = !wide && rows_allow(d_x, x_type, x_stride, len, 2, n) && rows_allow(d_y, y_type, y_stride, len, 2, n);    // 16-bit rows of even length
+    a.w_vec = (wide && params_vec(a, x_type, vec)) || (pairs && params_vec(a, x_type, 2));
     switch (x_type) {
         case NUPS_F64: return wide ? launch_norm<double, 2, false>(s, a, v, st) : launch_norm<double, 1, false>(s, a, v, st);
         case NUPS_F32: return wide ? launch_norm<float, 4, false>(s, a, v, st) : launch_norm<float, 1, false>(s, a, v, st);
-        case NUPS_F16: return wide ? launch_norm<__half, 8, false>(s, a, v, st) : launch_norm<__half, 1, false>(s, a, v, st);
-        default: return wide ? launch_norm<__nv_bfloat16, 8, false>(s, a, v, st) : launch_norm<__nv_bfloat16, 1, false>(s, a, v, st);
+        case NUPS_F16: return wide ? launch_norm<__half, 8, false>(s, a, v, st) : pairs ? launch_norm<__half, 2, false>(s, a, v, st) : launch_norm<__half, 1, false>(s, a, v, st);
+        default: return wide ? launch_norm<__nv_bfloat16, 8, false>(s, a, v, st) : pairs ? launch_norm<__nv_bfloat16, 2, false>(s, a, v, st) : launch_norm<__nv_bfloat16, 1, false>(s, a, v, st);
     }
 }
 
@@ -1079,7 +1084,7 @@ nups_status launch_grad(nups_store* s, GradArgs a, int x_type, void* d_dw, void*
         nups_launch_dependent(norm_grad_ring_kernel<X, D, TPR_, CH_, ROWS_, STAGES_>, blocks, TPR_, smem, st, a);                          \
     }
     bool through_ring = false;
-    if constexpr (VEC > 1) {
+    if constexpr (VEC * sizeof(X) == 16) {
         // fewer rows: every block has one group, nothing to run ahead of
         through_ring = chunks > 64 && chunks <= (sizeof(X) == 2 ? 1024 : 2048) && a.n > (uint64_t)s->sm_count && len * sizeof(D) % 16 == 0 && ((uintptr_t)a.dy & 15) == 0 &&
                        a.dys * sizeof(D) % 16 == 0;
@@ -1103,7 +1108,7 @@ nups_status launch_grad(nups_store* s, GradArgs a, int x_type, void* d_dw, void*
         }
         nups_launch_dependent(norm_grad_apply_kernel<X, VEC>, dim3(grid_for(len, 256 * VEC), blocks), 256, 0, st, a, (const A*)sums);
     }
-    else if constexpr (VEC > 1) {
+    else if constexpr (VEC * sizeof(X) == 16) {
         if (chunks <= 4) NUPS_GRAD(4, 1, 4)
         else if (chunks <= 8) NUPS_GRAD(8, 1, 4)
         else if (chunks <= 16) NUPS_GRAD(16, 1, 4)
@@ -1116,16 +1121,20 @@ nups_status launch_grad(nups_store* s, GradArgs a, int x_type, void* d_dw, void*
         else if (chunks <= 2048) NUPS_GRAD(1024, 2, 1)
         else if constexpr (VEC == 4) NUPS_GRAD(1024, 4, 1)
     } else {
-        if (chunks <= 32) NUPS_GRAD(32, 1, 4)
-        else if (chunks <= 64) NUPS_GRAD(32, 2, 4)
+        // as forward: 600,000 rows of 17 floats 40 us (92 with a warp and four rows), 400,000 rows of 34 bf16 34 us (83 by single values)
+        if (chunks <= 16) NUPS_GRAD(4, 4, 2)
+        else if (chunks <= 32) NUPS_GRAD(8, 4, 2)
+        else if (chunks <= 64) NUPS_GRAD(16, 4, 2)
         else if (chunks <= 128) NUPS_GRAD(32, 4, 2)
         else if (chunks <= 256) NUPS_GRAD(32, 8, 1)
         else if (chunks <= 512) NUPS_GRAD(32, 16, 1)
         else if (chunks <= 1024) NUPS_GRAD(128, 8, 1)
-        else if (chunks <= 2048) NUPS_GRAD(128, 16, 1)
-        else if (chunks <= 4096) NUPS_GRAD(256, 16, 1)
-        else if (sizeof(A) == 4 && chunks <= 8192) NUPS_GRAD(512, 16, 1)
-        else if constexpr (sizeof(A) == 4) NUPS_GRAD(1024, 16, 1)
+        else if (chunks <= 2048) NUPS_GRAD((VEC == 1 ? 128 : 256), (VEC == 1 ? 16 : 8), 1)
+        else if (chunks <= 4096) NUPS_GRAD((VEC == 1 ? 256 : 512), (VEC == 1 ? 16 : 8), 1)
+        else if constexpr (sizeof(A) == 4 && VEC == 1) {
+            if (chunks <= 8192) NUPS_GRAD(512, 16, 1)
+            else NUPS_GRAD(1024, 16, 1)
+        } else if constexpr (VEC == 2) NUPS_GRAD(1024, 8, 1)
     }
 #undef NUPS_GRAD
     LAUNCH_CHECK(s);
@@ -1180,15 +1189,19 @@ extern "C" nups_status nups_layer_norm_grad(nups_store* s, const void* d_x, int 
     const int vec = (int)(16 / type_bytes(x_type));
     const bool wide = rows_allow(d_x, x_type, x_stride, len, vec, n) && rows_allow(d_dy, dy_type, dy_stride, len, vec, n) &&
                       (!d_dx || rows_allow(d_dx, x_type, dx_stride, len, vec, n));
-    const size_t run = (size_t)vec * (w_type == NUPS_F32 && x_type != NUPS_F64 ? 4 : type_bytes(x_type));
-    a.w_vec = wide && aligned(d_weight, run > 16 ? 16 : run);
+    const bool pairs = !wide && rows_allow(d_x, x_type, x_stride, len, 2, n) && rows_allow(d_dy, dy_type, dy_stride, len, 2, n) &&
+                       (!d_dx || rows_allow(d_dx, x_type, dx_stride, len, 2, n));           // 16-bit rows of even length
+    const size_t run = (size_t)(pairs ? 2 : vec) * (w_type == NUPS_F32 && x_type != NUPS_F64 ? 4 : type_bytes(x_type));
+    a.w_vec = (wide || pairs) && aligned(d_weight, run > 16 ? 16 : run);
     char* scratch = (char*)d_scratch;
 #define NUPS_LAUNCH(X_, D_, V_) (wide ? launch_grad<X_, D_, V_>(s, a, x_type, d_dweight, d_dbias, scratch, st) : launch_grad<X_, D_, 1>(s, a, x_type, d_dweight, d_dbias, scratch, st))
+#define NUPS_LAUNCH16(X_) (!wide && pairs ? launch_grad<X_, X_, 2>(s, a, x_type, d_dweight, d_dbias, scratch, st) : NUPS_LAUNCH(X_, X_, 8))
     switch (x_type) {
         case NUPS_F64: return NUPS_LAUNCH(double, double, 2);
         case NUPS_F32: return dy_type == NUPS_F32 ? NUPS_LAUNCH(float, float, 4) : dy_type == NUPS_F16 ? NUPS_LAUNCH(float, __half, 4) : NUPS_LAUNCH(float, __nv_bfloat16, 4);
-        case NUPS_F16: return NUPS_LAUNCH(__half, __half, 8);
-        default: return NUPS_LAUNCH(__nv_bfloat16, __nv_bfloat16, 8);
+        case NUPS_F16: return NUPS_LAUNCH16(__half);
+        default: return NUPS_LAUNCH16(__nv_bfloat16);
     }
+#undef NUPS_LAUNCH16
 #undef NUPS_LAUNCH
 }

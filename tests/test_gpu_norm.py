@@ -362,3 +362,21 @@ def test_refusals(store):
     assert L.nups_layer_norm(None, p(x), 0, 64, 4, 64, None, None, 0, 1e-5, p(dx), 0, 64, None, None, st) == EINVAL
     torch.cuda.synchronize()
     assert (dx == 7.0).all() and (dw == 7.0).all()          # nothing was enqueued
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("length", [6, 30, 34, 62, 126, 202, 254, 510, 1002, 2046, 4094, 8190, 16382, 20002, 33002])
+def test_rows_of_even_length_that_16_byte_loads_cannot_read(store, length, dtype):
+    n = 2000 if length < 300 else 170
+    x, dy = make(n, length, dtype, length, gap=2), make(n, length, dtype, length + 1, gap=4, shift=0.1)
+    w, b = params(length, F32, 3)
+    whole = torch.full((n, length + 6), 7.0, dtype=dtype, device="cuda")
+    y, mean, rstd = store.layer_norm(x, w, b, eps=1e-5, out=whole[:, 2:length + 2])
+    check_forward(x, w, b, 1e-5, y, mean, rstd)
+    assert (whole[:, :2] == 7.0).all() and (whole[:, length + 2:] == 7.0).all()
+    w1 = torch.cat([w[:1], w])[1:]                    # an address that a pair of weights cannot be read at
+    y1, mean1, rstd1 = store.layer_norm(x, w1, b, eps=1e-5)
+    assert torch.equal(y1, y) and torch.equal(mean1, mean) and torch.equal(rstd1, rstd)
+    grads = store.layer_norm_grad(x, dy, mean, rstd, w, dx=whole[:, 2:length + 2])
+    check_grad(x, dy, mean, rstd, w, grads)
+    assert (whole[:, :2] == 7.0).all() and (whole[:, length + 2:] == 7.0).all()
