@@ -586,8 +586,15 @@ class Store:
         top, pdw = r.choice.shape[1], None
         if out.dtype != logits.dtype or r.choice.shape[0] != n or r.lse.shape[0] != n or r.counts.shape[0] != experts:
             raise NupsError(EINVAL, w, "out must have the logits' type, and the routing must be of these logits")
-        if r.counts.dtype != torch.int64 or r.tokens.dtype != torch.int64 or not (r.counts.is_cuda and r.tokens.is_cuda):
-            raise NupsError(EINVAL, w, "counts and tokens must be int64, on the store's device")
+        # a caller may have put other tensors in their place (sums over processes)
+        here = self._index
+        if r.counts.dtype != torch.int64 or r.tokens.dtype != torch.int64 or r.tokens.numel() != 1 or not r.counts.is_contiguous() or \
+                r.counts.get_device() != here or r.tokens.get_device() != here:
+            raise NupsError(EINVAL, w, "counts and tokens must be contiguous int64 on the store's device, tokens one value")
+        if r.weight.shape != r.choice.shape or r.weight.get_device() != here or r.lse.get_device() != here or \
+                not (r.choice.is_contiguous() and r.weight.is_contiguous() and r.lse.is_contiguous()) or \
+                r.choice.dtype != torch.int32 or r.weight.dtype != torch.float32 or r.lse.dtype != torch.float32:
+            raise NupsError(EINVAL, w, "choice, weight and lse must be as route gave them")
         if dweight is not None:
             if dweight.shape != r.choice.shape or dweight.dtype != torch.float32 or not dweight.is_contiguous():
                 raise NupsError(EINVAL, w, f"dweight must be a contiguous float32 {n} x {top}")

@@ -330,3 +330,16 @@ def test_choices_are_keys_of_a_store():
     order = sorted(range(E), key=lambda e: (-r.counts[e].item(), e))[:3]
     assert hot.tolist() == order
     assert torch.equal(s.pull(r.choice.view(-1))[:, 0].long(), r.choice.view(-1).long() * L)
+
+
+def test_routings_whose_tensors_were_replaced(store):
+    E = binding.EINVAL
+    x = make(8, 40, F32, 15)
+    r = store.route(x, 2, balance=0.01)
+    g = store.route_grad(x, r)
+    assert torch.equal(store.route_grad(x, r._replace(counts=r.counts.clone(), tokens=r.tokens.reshape(1))), g)
+    for other in (dict(counts=r.counts[:1].expand(40)), dict(counts=r.counts.repeat(2)[::2]), dict(counts=r.counts.int()), dict(counts=r.counts.cpu()),
+                  dict(tokens=r.tokens.cpu()), dict(tokens=r.counts), dict(choice=r.choice.long()), dict(choice=r.choice[:, :1].expand(8, 2)),
+                  dict(choice=r.choice[:, :1]), dict(weight=r.weight[:, :1].expand(8, 2)), dict(weight=r.weight.half()), dict(weight=r.weight.cpu()),
+                  dict(lse=r.lse[:1].expand(8)), dict(lse=r.lse.double()), dict(lse=r.lse.cpu())):
+        refused(E, lambda: store.route_grad(x, r._replace(**other)))
