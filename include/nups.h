@@ -400,9 +400,10 @@ nups_status nups_pull_norm(nups_store* store, const uint32_t* d_keys, uint64_t n
  *   dx = rstd (g - mean(g) - h mean(g h))      x's type, NULL: not wanted
  *   dweight = sum over rows of dy h            w_type, NULL: not wanted
  *   dbias = sum over rows of dy                w_type, NULL: not wanted
- * The sums over rows run in an order fixed by n, len and the type.  With n = 0
- * dweight and dbias are set to zero.  dx may be x or dy (same type and stride).
- * Scratch is needed when dweight or dbias is wanted.                           */
+ * The sums over rows run in an order fixed by n, len, the types and the rows'
+ * alignment.  With n = 0 dweight and dbias are set to zero.  dx may be x or dy
+ * (same type and stride).  Scratch is needed when dweight or dbias is wanted, and
+ * for rows of more than 16384 values (fp64: 4096).                             */
 nups_status nups_layer_norm_grad(nups_store* store, const void* d_x, int x_type, uint64_t x_stride, const void* d_dy, int dy_type,
                                  uint64_t dy_stride, uint64_t n, uint32_t len, const void* d_mean, const void* d_rstd,
                                  const void* d_weight, int w_type, void* d_dx, uint64_t dx_stride, void* d_dweight, void* d_dbias,

@@ -535,7 +535,8 @@ nups_status launch_norm(nups_store* s, const NormArgs& a, const View& v, cudaStr
     }
     if constexpr (VEC * sizeof(X) == 16) {
         // short rows: several teams to a warp with a few chunks per lane, one row each (1M pulled rows of 128 floats: 205 us with
-        // 8 lanes of 4 chunks, 209 with 16 of 2, two rows each, 278 with 32 of 1, four rows each)
+        // 8 lanes of 4 chunks, 209 with 16 of 2, two rows each, 278 with 32 of 1, four rows each;
+        // the lookups' running ahead took the first to 197)
         if (chunks <= 4) NUPS_NORM(4, 1, 2)
         else if (chunks <= 8) NUPS_NORM(4, 2, 1)
         else if (chunks <= 16) NUPS_NORM((VEC <= 4 ? 4 : 8), (VEC <= 4 ? 4 : 2), 1)
