@@ -486,16 +486,22 @@ template <class... KArgs> unsigned resident_blocks(void (*kernel)(KArgs...), int
     return n > 0 ? (unsigned)n : 1u;
 }
 
-// The same with dynamic shared memory, whose size the call decides; also asks for that much on the device.  What the last call with
-// this kernel found is remembered (device, size, blocks): the two queries take a microsecond.
-template <class... KArgs> unsigned ring_blocks(std::atomic<uint64_t>& last, int device, void (*kernel)(KArgs...), int block, size_t smem)
+// The same with dynamic shared memory.  `largest`, what the kernel's longest rows need, is asked for once per device: the limit is the
+// kernel's, not the call's, and another thread's call with shorter rows must not lower it between this call's asking and its launch.
+// The size of this call decides how many blocks fit; the last answer is remembered (device, size, blocks: one word, so that
+// threads see all of one answer), as the query takes half a microsecond.
+struct RingLimits { std::atomic<uint64_t> asked{0}, last{0}; };
+template <class... KArgs> unsigned ring_blocks(RingLimits& known, int device, void (*kernel)(KArgs...), int block, size_t largest, size_t smem)
 {
-    const uint64_t key = ((uint64_t)(device + 1) << 48) | ((uint64_t)smem << 16), seen = last.load(std::memory_order_relaxed);
+    if (device >= 64 || !(known.asked.load(std::memory_order_acquire) >> device & 1)) {
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)largest) != cudaSuccess) return 0;
+        if (device < 64) known.asked.fetch_or(1ull << device, std::memory_order_release);
+    }
+    const uint64_t key = ((uint64_t)(device + 1) << 48) | ((uint64_t)smem << 16), seen = known.last.load(std::memory_order_relaxed);
     if ((seen & ~0xFFFFull) == key) return (unsigned)(seen & 0xFFFF);
     int n = 0;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return 0;
     if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, block, smem) != cudaSuccess || n < 1) return 0;
-    last.store(key | (uint64_t)n, std::memory_order_relaxed);
+    known.last.store(key | (uint64_t)n, std::memory_order_relaxed);
     return (unsigned)n;
 }
 
@@ -506,9 +512,10 @@ nups_status launch_norm(nups_store* s, const NormArgs& a, const View& v, cudaStr
     const uint32_t chunks = (a.len + VEC - 1) / VEC;
 #define NUPS_RING(TPR_, CH_, ROWS_, STAGES_)                                                                                               \
     {                                                                                                                                      \
+        constexpr size_t largest = (size_t)STAGES_ * ROWS_ * TPR_ * CH_ * 16;                                                              \
         const size_t smem = (size_t)STAGES_ * ROWS_ * a.len * sizeof(X);                                                                   \
-        static std::atomic<uint64_t> last{0};                                                                                              \
-        const unsigned resident = ring_blocks(last, s->device, norm_ring_kernel<X, TPR_, CH_, ROWS_, STAGES_>, TPR_, smem);                \
+        static RingLimits known;                                                                                                           \
+        const unsigned resident = ring_blocks(known, s->device, norm_ring_kernel<X, TPR_, CH_, ROWS_, STAGES_>, TPR_, largest, smem);      \
         if (!resident) return nups_cuda_fail(cudaGetLastError(), "norm_ring_kernel");                                                      \
         const unsigned grid = grid_for(a.n, ROWS_, (unsigned)s->sm_count * resident);                                                      \
         nups_launch_dependent(norm_ring_kernel<X, TPR_, CH_, ROWS_, STAGES_>, grid, TPR_, smem, st, a);                                    \
@@ -1078,9 +1085,10 @@ nups_status launch_grad(nups_store* s, GradArgs a, int x_type, void* d_dw, void*
     }
 #define NUPS_GRAD_RING(TPR_, CH_, ROWS_, STAGES_)                                                                                           \
     {                                                                                                                                      \
+        constexpr size_t largest = (size_t)STAGES_ * ROWS_ * TPR_ * CH_ * VEC * (sizeof(X) + sizeof(D));                                   \
         const size_t smem = (size_t)STAGES_ * ROWS_ * len * (sizeof(X) + sizeof(D));                                                       \
-        static std::atomic<uint64_t> last{0};                                                                                              \
-        if (!ring_blocks(last, s->device, norm_grad_ring_kernel<X, D, TPR_, CH_, ROWS_, STAGES_>, TPR_, smem))                             \
+        static RingLimits known;                                                                                                           \
+        if (!ring_blocks(known, s->device, norm_grad_ring_kernel<X, D, TPR_, CH_, ROWS_, STAGES_>, TPR_, largest, smem))                   \
             return nups_cuda_fail(cudaGetLastError(), "norm_grad_ring_kernel");                                                            \
         nups_launch_dependent(norm_grad_ring_kernel<X, D, TPR_, CH_, ROWS_, STAGES_>, blocks, TPR_, smem, st, a);                          \
     }

@@ -6,6 +6,8 @@ magnitudes, a variance by some 90 u of itself (its terms' roundings and the mean
 covers the few roundings that follow.  A sum over rows: at most 32 rows per team one after the other, 32 sums of blocks, trees
 of 32: COLUMN_STEPS = 160 with the roundings of the terms.  The last rounding to the output's type adds half a step of it.
 """
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -380,3 +382,34 @@ def test_rows_of_even_length_that_16_byte_loads_cannot_read(store, length, dtype
     grads = store.layer_norm_grad(x, dy, mean, rstd, w, dx=whole[:, 2:length + 2])
     check_grad(x, dy, mean, rstd, w, grads)
     assert (whole[:, :2] == 7.0).all() and (whole[:, length + 2:] == 7.0).all()
+
+
+@pytest.mark.parametrize("backward", [False, True])
+def test_two_threads_with_a_store_each_and_rows_of_two_lengths(backward):
+    # both lengths take one kernel, with rings of different sizes.  The C interface itself, so that the threads are in it most of the time
+    failures, start = [], threading.Barrier(2)
+
+    def work(length):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            s = binding.Store(64, 64)
+            x, out = make(300, length, BF16, length), torch.empty((300, length), dtype=BF16, device="cuda")
+            mean, rstd = stats_of(x)
+            L, st, kind = s._l, torch.cuda.current_stream().cuda_stream, binding.TYPES[BF16]
+            px, po, pm, pr = (t.data_ptr() for t in (x, out, mean, rstd))
+            if backward:
+                fn, args = L.nups_layer_norm_grad, (s._s, px, kind, length, px, kind, length, 300, length, pm, pr, None, kind, po, length, None, None, None, 0, st)
+            else:
+                fn, args = L.nups_layer_norm, (s._s, px, kind, length, 300, length, None, None, kind, 1e-5, po, kind, length, None, None, st)
+            start.wait(60)
+            refused = sum(fn(*args) != 0 for _ in range(20_000))
+            torch.cuda.current_stream().synchronize()
+            want = s.layer_norm_grad(x, x, mean, rstd, need_params=False)[0] if backward else s.layer_norm(x, stats=False)
+            if refused or not torch.equal(out, want):
+                failures.append((length, refused))
+
+    threads = [threading.Thread(target=work, args=(length,)) for length in (4096, 2304)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failures
