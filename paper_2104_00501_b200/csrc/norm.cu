@@ -295,10 +295,11 @@ __global__ void __launch_bounds__(team_block(TPR)) norm_kernel(NormArgs a, View 
 #pragma unroll
                 for (int k = 0; k < ROWS; ++k) {
                     const uint64_t row = base + k * TEAMS + team;
-                    const A off = -mean[k] * rstd[k];
+                    const A minus = -mean[k];
                     A y[VEC];
                     unpack<A>(x[k][c], y);
-                    run_fma<VEC, false, true, true>(y, y, &rstd[k], &off);
+                    run_add<VEC, true>(y, y, &minus);       // x - mean first: x rstd - mean rstd would leave the roundings of both products
+                    run_scale<VEC>(y, y, rstd[k]);
                     run_fma<VEC, false, false, false>(y, y, HOLD ? w[c] : wc[0], HOLD ? b[c] : bc[0]);
                     if (row < a.n) store_chunk<X, A, VEC>(a.y, a.y_type, row * a.ys + at, y);
                 }
@@ -382,10 +383,11 @@ __global__ void __launch_bounds__(TPR) norm_ring_kernel(NormArgs a)
                 }
 #pragma unroll
                 for (int k = 0; k < ROWS; ++k) {
-                    const A off = -mean[k] * rstd[k];
+                    const A minus = -mean[k];
                     A y[VEC];
                     get(k, c, y);
-                    run_fma<VEC, false, true, true>(y, y, &rstd[k], &off);
+                    run_add<VEC, true>(y, y, &minus);       // as in norm_kernel
+                    run_scale<VEC>(y, y, rstd[k]);
                     run_fma<VEC, false, false, false>(y, y, HOLD ? w[c] : wc[0], HOLD ? b[c] : bc[0]);
                     if (base + k < a.n) store_chunk<X, A, VEC>(a.y, a.y_type, (base + k) * a.ys + at, y);
                 }

@@ -413,3 +413,50 @@ def test_two_threads_with_a_store_each_and_rows_of_two_lengths(backward):
     for t in threads:
         t.join()
     assert not failures
+
+
+def by_its_statistics(x, w, b, y, mean, rstd):
+    """y from the statistics that the call gave: x - mean, rstd, weight and bias are four operations, each off by half a unit of its own
+    result, so y is off by 4 units of the difference's part and one of itself.  Rows of equal values whose mean is exact give the bias."""
+    h = (x.double() - mean.double()[:, None]) * rstd.double()[:, None]
+    h = h if w is None else h * w.double()
+    b = torch.zeros_like(x[0]).double() if b is None else b.double()
+    u = unit(x.dtype)
+    tol = u * (4 * h.abs() + 2 * (h + b).abs()) + half_step(y.dtype) * (1 + u) * (h + b).abs() + tiny(y.dtype)
+    off = (y.double() - (h + b)).abs()
+    assert (off <= tol).all(), (off / tol).max()
+
+
+LEVELS = {F32: (1001.0, -12345.0, 100.0, 0.1, 5000.25), F64: (1001.0, -12345.0, 1e9 + 1, 0.1, 5000.25), F16: (1001.0, -1234.0, 100.0, 0.1, 500.25), BF16: (200.0, -1248.0, 100.0, 0.1, 5.25)}
+
+
+@pytest.mark.parametrize("dtype", [F32, F64, F16, BF16])
+@pytest.mark.parametrize("n,length", [(5, 1), (7, 2), (40, 16), (40, 33), (9, 100), (20, 128), (6, 300), (11, 500), (6, 1000), (5, 2050), (4, 4096), (3, 8200), (2, 20000),
+                                      (400, 640), (400, 1024), (320, 2048), (320, 4096), (170, 8192), (160, 16384)])
+def test_rows_whose_mean_is_large_against_their_deviation(store, n, length, dtype):
+    x = make(n, length, dtype, 31)
+    for k, level in enumerate(LEVELS[dtype]):
+        x[k::11] = level
+        x[k + 5::11] += level
+    w, b = params(length, dtype, 32)
+    for weight, bias in ((w, b), (None, None)):
+        y, mean, rstd = store.layer_norm(x, weight, bias)
+        by_its_statistics(x, weight, bias, y, mean, rstd)
+        if length <= 1024:                                  # sums of equal values of at most 14 bits are exact
+            for k, level in enumerate(LEVELS[dtype][:3]):
+                want = torch.zeros_like(y[k::11]) if bias is None else bias.expand_as(y[k::11])
+                assert torch.equal(mean[k::11].double(), x[k::11, 0].double()) and torch.equal(y[k::11], want)
+
+
+@pytest.mark.parametrize("value_bytes,length,out", [(4, 4, F32), (4, 128, BF16), (4, 1000, F32), (8, 100, F64), (4, 20000, F32)])
+def test_pulled_rows_whose_mean_is_large_against_their_deviation(value_bytes, length, out):
+    s = binding.Store(60, length, value_bytes=value_bytes)
+    table = make(60, length, s.dtype, 33)
+    table[::3] += 4000.0
+    table[1::3] = 1001.0
+    s.write_table(0, table.cpu().numpy())
+    w, b = params(length, s.dtype, 34)
+    y, mean, rstd, rows = s.pull_norm(dev_keys(range(60)), w, b, out_dtype=out, rows=True)
+    assert torch.equal(rows, table)
+    by_its_statistics(rows, w, b, y, mean, rstd)
+    s.close()
