@@ -460,3 +460,15 @@ def test_pulled_rows_whose_mean_is_large_against_their_deviation(value_bytes, le
     assert torch.equal(rows, table)
     by_its_statistics(rows, w, b, y, mean, rstd)
     s.close()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_very_long_rows_of_equal_values(store, dtype):
+    # a thread adds 16,384 or 32,768 values of such a row
+    x = torch.full((2, 1 << 25), 0.1, dtype=dtype, device="cuda")
+    x[1, ::2] = 0.3
+    y, mean, rstd = store.layer_norm(x)
+    check_forward(x, None, None, 1e-5, y, mean, rstd)
+    dy = torch.full_like(x, 0.1)
+    dy[1, ::2] = -0.2
+    check_grad(x, dy, mean, rstd, None, store.layer_norm_grad(x, dy, mean, rstd, need_params=False))
