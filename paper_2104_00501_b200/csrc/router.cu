@@ -41,6 +41,12 @@ template <int TPR> __device__ __forceinline__ float lanes_sum(float x)
     for (int o = TPR / 2; o > 0; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
     return x;
 }
+template <int TPR> __device__ __forceinline__ float lanes_most(float x)
+{
+#pragma unroll
+    for (int o = TPR / 2; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, o));
+    return x;
+}
 template <int TPR> __device__ __forceinline__ uint32_t lanes_max(uint32_t x)
 {
     if constexpr (TPR == 32) {
@@ -518,8 +524,15 @@ __global__ void __launch_bounds__(ROUTE_BLOCK) route_grad_kernel(RouteGradArgs a
         }
         float p[EPT];                                       // logits, then probabilities
         read_logits<X, VEC, TPR, EPT>(raw, on, a.experts, t, p);
-        float along[2] = {0, 0};
-        exponentials<EPT>(p, lse, p);
+        // p about the largest logit, as forward: lse is rounded at its own size, and e^(logit - lse) would carry that rounding in every p
+        float most = -CUDART_INF_F, two_sums[2] = {0, 0}, along[2] = {0, 0};
+#pragma unroll
+        for (int i = 0; i < EPT; ++i) most = fmaxf(most, p[i]);             // passes over NaN, which the sum shows
+        most = lanes_most<TPR>(most);
+        exponentials<EPT>(p, most == -CUDART_INF_F ? 0.0f : most, p);
+        sum_run<EPT>(two_sums, p);
+        const float total = lanes_sum<TPR>(two_sums[0] + two_sums[1]);
+        run_scale<EPT>(p, p, total == 0.0f ? 0.0f : 1.0f / total);          // 0: nothing but -infinity
         sum_run_of_products<EPT>(along, p, g);
         part += along[0] + along[1];
         const float off = zf * lse - lanes_sum<TPR>(part);

@@ -343,3 +343,34 @@ def test_routings_whose_tensors_were_replaced(store):
                   dict(choice=r.choice[:, :1]), dict(weight=r.weight[:, :1].expand(8, 2)), dict(weight=r.weight.half()), dict(weight=r.weight.cpu()),
                   dict(lse=r.lse[:1].expand(8)), dict(lse=r.lse.double()), dict(lse=r.lse.cpu())):
         refused(E, lambda: store.route_grad(x, r._replace(**other)))
+
+
+@pytest.mark.parametrize("shift", [100.0, -6016.0, 60000.0])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("n,experts,top", [(40, 12, 2), (33, 64, 4), (50, 100, 8), (60, 256, 8), (21, 333, 3), (12, 1000, 6)])
+def test_logits_far_from_zero(store, n, experts, top, dtype, shift):
+    # softmax, choices and gradients depend on the logits' differences alone: the bounds hold no part of the logits' own size
+    if dtype == F32:
+        x = (make(n, experts, F32, 51) * 64).round() / 64 + shift           # exact
+    else:
+        x = (make(n, experts, F32, 51) + shift).to(dtype)                   # few values, many equal ones
+    for renormalize in (False, True):
+        got = check(store, x, top, renormalize=renormalize)
+    if dtype == F32:                                        # the same differences give the same gradient, whatever the level (z = 0)
+        dw = torch.randn((n, top), device="cuda")
+        near, far = store.route(x - shift, top, balance=0.5), store.route(x, top, balance=0.5)
+        assert torch.equal(near.choice, far.choice) and torch.equal(near.weight, far.weight)
+        assert torch.equal(store.route_grad(x - shift, near, dweight=dw), store.route_grad(x, far, dweight=dw))
+
+
+def test_nan_and_infinity_stay_in_their_items_backward(store):
+    x, dw = make(40, 30, F32, 52), torch.randn((40, 3), device="cuda")
+    r = store.route(x, 3, balance=1.0, z=0.1)
+    clean = store.route_grad(x, r, dweight=dw)
+    others = [i for i in range(40) if i not in (7, 9, 11)]
+    y = x.clone()
+    y[7, 4], y[9, 4] = float("nan"), float("inf")
+    y[11] = -float("inf")
+    y[11, 2] = float("nan")
+    d = store.route_grad(y, r, dweight=dw)
+    assert d[[7, 9, 11]].isnan().all() and torch.equal(d[others], clean[others])
