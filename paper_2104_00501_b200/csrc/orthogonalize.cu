@@ -80,6 +80,14 @@ template <int N> __device__ __forceinline__ double sum_of_squares(const float* v
     for (int i = 0; i < N; ++i) sum = fmaf(v[i] * f, v[i] * f, sum);
     return (double)sum * __hiloint2double((1023 + 2 * (127 - e)) << 20, 0);
 }
+// Factors that bring a matrix whose squares sum to `sum` to X: X_SCALE / (norm + eps), which may lie outside fp32's range (zeros and a
+// tiny eps gave 0 times infinity), as a power of two and the rest, applied one after the other.
+__device__ __forceinline__ float2 first_factors(double sum, float eps)
+{
+    const double f = (double)X_SCALE / (sqrt(sum) + (double)eps);         // 2^-130 (65536 x 65536 of the largest float) to 2^163
+    const float power = f > 0x1p100 ? 0x1p100f : f < 0x1p-100 ? 0x1p-60f : 1.0f;
+    return make_float2(power, (float)(f / (double)power));
+}
 __device__ __forceinline__ double warp_sum_f64(double x)
 {
 #pragma unroll
@@ -179,16 +187,16 @@ __global__ void __launch_bounds__(SMALL_BLOCK) orthogonalize_small_kernel(OrthAr
     sum = 0;
 #pragma unroll
     for (int w = 0; w < SMALL_BLOCK / 32; ++w) sum += sums[w];
-    const float inv = (float)((double)X_SCALE / (sqrt(sum) + (double)a.eps));
+    const float2 f = first_factors(sum, a.eps);
     each_row([&](uint32_t r, const float (&v)[SMALL_N / 64][2]) {
 #pragma unroll
         for (int k = 0; k < SMALL_N / 64; ++k) {
             const uint32_t c = 2 * lane + 64 * k;
             if (c >= a.cols) continue;                      // what is beyond the matrix is zero, as it was
-            const float x = v[k][0] * inv, y = v[k][1] * inv;
+            const float x = v[k][0] * f.x * f.y, y = v[k][1] * f.x * f.y;
             const __half2 hi = __floats2half2_rn(x, y);
-            const float2 f = __half22float2(hi);
-            const __half2 lo = __floats2half2_rn(x - f.x, y - f.y);
+            const float2 h = __half22float2(hi);
+            const __half2 lo = __floats2half2_rn(x - h.x, y - h.y);
             if (!a.tall) {
                 const uint32_t at = panel_at(r, c);
                 *(__half2*)(x_hi + at) = hi;
@@ -405,7 +413,7 @@ __global__ void __launch_bounds__(256) orth_split_kernel(OrthArgs a, Planes p)
     sum = 0;
 #pragma unroll
     for (int w = 0; w < 8; ++w) sum += part[w];
-    const float f = (float)((double)X_SCALE / (sqrt(sum) + (double)a.eps));
+    const float2 f = first_factors(sum, a.eps);
     __half* hi = p.x[0] + (uint64_t)blockIdx.z * 2 * a.m * p.ldx;
     __half* lo = hi + (uint64_t)a.m * p.ldx;
 #pragma unroll
@@ -413,7 +421,7 @@ __global__ void __launch_bounds__(256) orth_split_kernel(OrthArgs a, Planes p)
         const uint32_t r = r0 + ty + 4 * k, c = c0 + tx;
         if (r < a.m && c < a.n) {
             __half h, l;
-            split((a.tall ? tile[ty + 4 * k][tx] : v[k]) * f, h, l);
+            split((a.tall ? tile[ty + 4 * k][tx] : v[k]) * f.x * f.y, h, l);
             hi[(uint64_t)r * p.ldx + c] = h;
             lo[(uint64_t)r * p.ldx + c] = l;
         }

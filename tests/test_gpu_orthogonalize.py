@@ -226,3 +226,15 @@ def test_a_step_of_rows_that_hold_matrices():
     want[at.long()] -= rate * ref.reshape(3, r * c)
     s.sync()
     assert (s.read_table().double() - want).abs().max() <= 1e-4 * rate + 2.0 ** -24 * want.abs().max()
+
+
+@pytest.mark.parametrize("rows,cols", [(20, 30), (30, 20), (150, 170), (170, 150)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_zeros_and_tiny_matrices_with_a_tiny_eps(store, rows, cols, dtype):
+    zeros = torch.zeros((2, rows, cols), dtype=dtype, device="cuda")
+    for eps in (1e-30, 1e-35, 1e-38, 1e-44):
+        assert not store.orthogonalize(zeros, eps=eps).any()
+    for power in (-110, -123, -132):                        # norms of 2^-109 to 2^-131 or so, many of the values below the normal range
+        g = (make(2, rows, cols, F64, 61) * 2.0 ** power).to(dtype)
+        for eps in (1e-42, 1e-37):
+            check(store, g, eps=float(np.float32(eps)))
