@@ -897,28 +897,27 @@ nups_status launch_large(nups_store* s, const OrthArgs& o, uint32_t batch, char*
     return NUPS_OK;
 }
 
-// Does the iteration stay within the range of the pairs for singular values in [0, 1]?
-bool coefficients_fit(const float* c, uint32_t steps)
+// Does the iteration stay within the range of the pairs for singular values in [0, 1]?  p(s) = s (a + b s^2 + c s^4) takes [0, top] to an
+// interval that begins at 0, so a step's largest value is that of |p| at top or where p' = a + 3 b u + 5 c u^2, u = s^2, is zero,
+// and the factor's is at 0, at top or at u = -b / 2c.  Exact for all singular values; samples of them missed the few that run away.
+bool coefficients_fit(const float* h, uint32_t steps)
 {
-    constexpr int POINTS = 512;
-    // the answer for the thread's last coefficients: a program has one set of them, and working it out takes 5 us
-    thread_local float seen[3] = {0, 0, 0};
-    thread_local uint32_t seen_steps = 0;
-    thread_local bool fits = false;
-    if (!isfinite(c[0]) || !isfinite(c[1]) || !isfinite(c[2])) return false;
-    if (seen_steps == steps && seen[0] == c[0] && seen[1] == c[1] && seen[2] == c[2]) return fits;
-    fits = true;
-    for (int i = 0; fits && i <= POINTS; ++i) {
-        double x = (double)i / POINTS;
-        for (uint32_t k = 0; fits && k < steps; ++k) {
-            const double x2 = x * x, f = c[0] + x2 * (c[1] + x2 * c[2]);
-            x = fabs(x * f);
-            fits = fabs(f) <= 7.5 && x <= 2.5;
-        }
+    const double a = h[0], b = h[1], c = h[2];
+    if (!isfinite(a) || !isfinite(b) || !isfinite(c)) return false;
+    auto factor = [&](double u) { return fabs(a + u * (b + u * c)); };
+    // zeros of q(u) = a + 3 b u + 5 c u^2, by the form that does not cancel; none: infinity or NaN, which the bounds below leave out
+    const double root = sqrt(9 * b * b - 20 * a * c), q = -1.5 * b - copysign(0.5 * root, b);
+    const double turns[2] = {q / (5 * c), a / q}, bend = -b / (2 * c);
+    double top = 1.0;                                       // largest square of a singular value
+    for (uint32_t k = 0; k < steps; ++k) {
+        double f = fmax(factor(0.0), factor(top)), s = sqrt(top) * factor(top);
+        if (bend > 0 && bend < top) f = fmax(f, factor(bend));
+        for (double u : turns)
+            if (u > 0 && u < top) s = fmax(s, sqrt(u) * factor(u));
+        if (!(f <= 7.5) || !(s <= 2.5)) return false;
+        top = s * s;
     }
-    for (int i = 0; i < 3; ++i) seen[i] = c[i];
-    seen_steps = steps;
-    return fits;
+    return true;
 }
 
 bool matrix_fits(uint64_t stride, uint64_t batch_stride, uint32_t batch, uint32_t rows, uint32_t cols)

@@ -238,3 +238,18 @@ def test_zeros_and_tiny_matrices_with_a_tiny_eps(store, rows, cols, dtype):
         g = (make(2, rows, cols, F64, 61) * 2.0 ** power).to(dtype)
         for eps in (1e-42, 1e-37):
             check(store, g, eps=float(np.float32(eps)))
+
+
+def test_coefficients_that_send_a_few_singular_values_out_of_range(store):
+    # a singular value of 0.9968385 leaves every bound in eight steps; values a thousandth to either side do not
+    c, s = (2.77, -5.98, 2.19), 0.9968385
+    refused(binding.EINVAL, lambda: store.orthogonalize(torch.diag(torch.tensor([s, (1 - s * s) ** 0.5], device="cuda")), steps=8, coefficients=c))
+    # 2.5 and 7.5 themselves, and what lies just beyond
+    g = make(1, 10, 20, F32, 62)
+    for good, bad in (((2.5, 0.0, 0.0), (2.5001, 0.0, 0.0)), ((7.5, -11.0, 3.0), (7.501, -11.0, 3.0)), ((0.0, 2.5, 0.0), (0.0, -2.501, 0.0))):
+        store.orthogonalize(g, steps=1, coefficients=good)
+        refused(binding.EINVAL, lambda: store.orthogonalize(g, steps=1, coefficients=bad))
+    for steps in (1, 5, 64):
+        store.orthogonalize(g, steps=steps)
+        store.orthogonalize(g, steps=steps, coefficients=(1.5, -0.5, 0.0))
+        store.orthogonalize(g, steps=steps, coefficients=(2.0, -1.5, 0.5))
