@@ -310,7 +310,7 @@ __global__ void __launch_bounds__(SMALL_BLOCK) orthogonalize_small_kernel(OrthAr
             sum_runs(c0, n16, m16 / 16, v);
             if (last) {
 #pragma unroll
-                for (int j = 0; j < 32; ++j) v[j] *= FROM_BX * a.scale;
+                for (int j = 0; j < 32; ++j) v[j] = v[j] * FROM_BX * a.scale;       // their product may be below the normal range
                 if (!ok || quarter >= a.m || c0 >= a.n) continue;          // ok: the same for all threads but after a second's wait in vain
                 if (!a.tall) {
                     write_rows(out, TYPE, (uint64_t)quarter * a.os + c0, a.os, a.m - quarter, a.n - c0, v, (float*)base + warp * 32 * 33);
@@ -627,9 +627,8 @@ orth_tiled_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         const uint32_t col = col0 + own_col;
         if (MODE == LAST || MODE == PART) {
             float* tile = (float*)base + (warp - 2) * 32 * 33;
-            const float f = MODE == PART ? FROM_XX * A_SCALE : FROM_BX * o.scale;
 #pragma unroll
-            for (int j = 0; j < OWN; ++j) acc[j] *= f;
+            for (int j = 0; j < OWN; ++j) acc[j] = MODE == PART ? acc[j] * (FROM_XX * A_SCALE) : acc[j] * FROM_BX * o.scale;
 #pragma unroll
             for (int c = 0; c < OWN; c += 32) {
                 if (!ok || row0 + quarter >= t.m || col + c >= t.n) continue;

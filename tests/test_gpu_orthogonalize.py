@@ -253,3 +253,12 @@ def test_coefficients_that_send_a_few_singular_values_out_of_range(store):
         store.orthogonalize(g, steps=steps)
         store.orthogonalize(g, steps=steps, coefficients=(1.5, -0.5, 0.0))
         store.orthogonalize(g, steps=steps, coefficients=(2.0, -1.5, 0.5))
+
+
+@pytest.mark.parametrize("rows,cols", [(20, 30), (150, 170), (170, 150)])
+def test_tiny_and_huge_scales(store, rows, cols):
+    # the iterate is brought to its size by a power of two, then multiplied: one rounding
+    g = make(2, rows, cols, F32, 63)
+    want = store.orthogonalize(g)
+    for scale in (-0.02, 1e-25, -3e-31, 7e-36, 1e30, -3e38):
+        assert torch.equal(store.orthogonalize(g, scale=scale), want * torch.tensor(scale, device="cuda"))
