@@ -584,14 +584,14 @@ nups_status launch_norm(nups_store* s, const NormArgs& a, const View& v, cudaStr
     return NUPS_OK;
 }
 
-bool aligned(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
+size_t stat_bytes(int x_type) { return x_type == NUPS_F64 ? 8 : 4; }
 
 // weight and bias may be read VEC values at a time
 int params_vec(const NormArgs& a, int x_type, int vec)
 {
     const size_t run = (size_t)vec * (a.w_type == NUPS_F32 && x_type != NUPS_F64 ? 4 : type_bytes(x_type));
     const size_t need = run > 16 ? 16 : run;
-    return aligned(a.w, need) && aligned(a.b, need);
+    return suits(need, a.w, a.b);
 }
 
 bool w_type_fits(int x_type, int w_type) { return w_type == x_type || (w_type == NUPS_F32 && x_type != NUPS_F64); }
@@ -602,7 +602,7 @@ bool eps_fits(int x_type, double eps) { return eps > 0 && eps < 1e30 && (x_type 
 bool rows_allow(const void* p, int type, uint64_t stride, uint32_t len, int vec, uint64_t n)
 {
     const size_t run = type_bytes(type) * vec, need = run > 16 ? 16 : run;
-    return len % vec == 0 && aligned(p, need) && (n <= 1 || stride % vec == 0);
+    return len % vec == 0 && suits(need, p) && (n <= 1 || stride % vec == 0);
 }
 
 }  // namespace
@@ -615,6 +615,9 @@ extern "C" nups_status nups_layer_norm(nups_store* s, const void* d_x, int x_typ
     if (len == 0 || len >= (1u << 28) || n >= (1ull << 32) || (n > 1 && (x_stride < len || y_stride < len))) return NUPS_EINVAL;
     if (x_stride >= (1ull << 32) || y_stride >= (1ull << 32)) return NUPS_EINVAL;
     if (n && (!d_x || !d_y)) return NUPS_EINVAL;
+    if (!suits(type_bytes(x_type), d_x) || !suits(type_bytes(y_type), d_y) || !suits(type_bytes(w_type), d_weight, d_bias) ||
+        !suits(stat_bytes(x_type), d_mean, d_rstd))
+        return NUPS_EINVAL;
     nups_status rc = on_own_device(s);
     if (rc != NUPS_OK || n == 0) return rc;
     NormArgs a = {d_x, x_stride, d_y, y_stride, d_weight, d_bias, d_mean, d_rstd, n, len, y_type, w_type, 0, eps, nullptr, nullptr, s->st};
@@ -638,7 +641,7 @@ extern "C" nups_status nups_pull_norm(nups_store* s, const uint32_t* d_keys, uin
     if (!s) return NUPS_EINVAL;
     const int type = s->vb == 8 ? NUPS_F64 : NUPS_F32;
     if (!other_type_fits(type, y_type) || !eps_fits(type, eps) || n >= (1ull << 32) || (n && (!d_keys || !d_y))) return NUPS_EINVAL;
-    if (!aligned(d_y, 16) || !aligned(d_rows, 16)) return NUPS_EINVAL;
+    if (!suits(16, d_y, d_rows) || !suits(4, d_keys) || !suits(type_bytes(type), d_weight, d_bias, d_mean, d_rstd)) return NUPS_EINVAL;
     nups_status rc = on_own_device(s);
     if (rc != NUPS_OK || n == 0) return rc;
     NormArgs a = {s->val, s->value_len, d_y, s->value_len, d_weight, d_bias, d_mean, d_rstd, n, s->value_len, y_type, type, 0, eps, d_keys, d_rows, s->st};
@@ -1188,11 +1191,14 @@ extern "C" nups_status nups_layer_norm_grad(nups_store* s, const void* d_x, int 
     if (len == 0 || len >= (1u << 28) || n >= (1ull << 32) || (n > 1 && (x_stride < len || dy_stride < len || (d_dx && dx_stride < len)))) return NUPS_EINVAL;
     if (x_stride >= (1ull << 32) || dy_stride >= (1ull << 32) || dx_stride >= (1ull << 32)) return NUPS_EINVAL;
     if (n && (!d_x || !d_dy || !d_mean || !d_rstd)) return NUPS_EINVAL;
+    if (!suits(type_bytes(x_type), d_x, d_dx) || !suits(type_bytes(dy_type), d_dy) || !suits(type_bytes(w_type), d_weight, d_dweight, d_dbias) ||
+        !suits(stat_bytes(x_type), d_mean, d_rstd))
+        return NUPS_EINVAL;
     const bool sums = d_dweight || d_dbias;
     const bool needs = n && (sums || (d_dx && len > grad_long_from(x_type)));
     uint64_t bytes = 0;
     nups_layer_norm_grad_scratch(s, n, len, x_type, &bytes);
-    if (needs && (!d_scratch || scratch_bytes < bytes || !aligned(d_scratch, 256))) return NUPS_EINVAL;
+    if (needs && (!d_scratch || scratch_bytes < bytes || !suits(256, d_scratch))) return NUPS_EINVAL;
     nups_status rc = on_own_device(s);
     if (rc != NUPS_OK) return rc;
     cudaStream_t st = (cudaStream_t)stream;
@@ -1209,7 +1215,7 @@ extern "C" nups_status nups_layer_norm_grad(nups_store* s, const void* d_x, int 
     const bool pairs = !wide && rows_allow(d_x, x_type, x_stride, len, 2, n) && rows_allow(d_dy, dy_type, dy_stride, len, 2, n) &&
                        (!d_dx || rows_allow(d_dx, x_type, dx_stride, len, 2, n));           // 16-bit rows of even length
     const size_t run = (size_t)(pairs ? 2 : vec) * (w_type == NUPS_F32 && x_type != NUPS_F64 ? 4 : type_bytes(x_type));
-    a.w_vec = (wide || pairs) && aligned(d_weight, run > 16 ? 16 : run);
+    a.w_vec = (wide || pairs) && suits(run > 16 ? 16 : run, d_weight);
     char* scratch = (char*)d_scratch;
 #define NUPS_LAUNCH(X_, D_, V_) (wide ? launch_grad<X_, D_, V_>(s, a, x_type, d_dweight, d_dbias, scratch, st) : launch_grad<X_, D_, 1>(s, a, x_type, d_dweight, d_dbias, scratch, st))
 #define NUPS_LAUNCH16(X_) (!wide && pairs ? launch_grad<X_, X_, 2>(s, a, x_type, d_dweight, d_dbias, scratch, st) : NUPS_LAUNCH(X_, X_, 8))

@@ -11,6 +11,9 @@
 static inline bool type_known(int t) { return t == NUPS_F32 || t == NUPS_F64 || t == NUPS_F16 || t == NUPS_BF16; }
 static inline size_t type_bytes(int t) { return t == NUPS_F64 ? 8 : t == NUPS_F32 ? 4 : 2; }
 
+// Are these addresses (NULL included) multiples of `bytes`, a power of two?  Kernels read and write whole values.
+template <class... P> static inline bool suits(size_t bytes, const P*... p) { return ((... | (uintptr_t)p) & (bytes - 1)) == 0; }
+
 // Does the call's current device hold the store?  Kernels are launched on the current device, on a stream of it.
 static inline nups_status on_own_device(const nups_store* s)
 {

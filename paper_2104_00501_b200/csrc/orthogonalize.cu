@@ -946,7 +946,7 @@ extern "C" nups_status nups_orthogonalize(nups_store* s, const void* d_update, i
     if (steps < 1 || steps > NUPS_ORTHOGONALIZE_MAX_STEPS || !h_coefficients || !coefficients_fit(h_coefficients, steps) || !(eps > 0) || !isfinite(eps) || !isfinite(scale))
         return NUPS_EINVAL;
     if (!matrix_fits(stride, batch_stride, batch, rows, cols) || !matrix_fits(out_stride, out_batch_stride, batch, rows, cols)) return NUPS_EINVAL;
-    if (batch && (!d_update || !d_out)) return NUPS_EINVAL;
+    if ((batch && (!d_update || !d_out)) || !suits(type_bytes(type), d_update, d_out)) return NUPS_EINVAL;
     if (batch && bytes && (!d_scratch || scratch_bytes < bytes || ((uintptr_t)d_scratch & 255))) return NUPS_EINVAL;
     nups_status rc = on_own_device(s);
     if (rc != NUPS_OK || batch == 0) return rc;

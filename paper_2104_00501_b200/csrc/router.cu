@@ -698,6 +698,7 @@ extern "C" nups_status nups_route(nups_store* s, const void* d_logits, int type,
 {
     if (!s || !route_sizes(type, stride, n, experts, top, balance, z) || !d_counts || !d_tokens) return NUPS_EINVAL;
     if (n && (!d_logits || !d_choice || !d_weight)) return NUPS_EINVAL;
+    if (!suits(type_bytes(type), d_logits) || !suits(4, d_choice, d_weight, d_lse, d_prob, d_loss) || !suits(8, d_counts, d_tokens)) return NUPS_EINVAL;
     uint64_t bytes = 0;
     nups_route_scratch(s, n, experts, &bytes);
     if (bytes && (!d_scratch || scratch_bytes < bytes || ((uintptr_t)d_scratch & 255))) return NUPS_EINVAL;
@@ -724,6 +725,7 @@ extern "C" nups_status nups_route_grad(nups_store* s, const void* d_logits, int 
 {
     if (!s || !route_sizes(type, stride, n, experts, top, balance, z) || !route_sizes(type, dlogits_stride, n, experts, top, 0, 0)) return NUPS_EINVAL;
     if (n && (!d_logits || !d_lse || !d_counts || !d_tokens || !d_dlogits || (d_dweight && (!d_choice || !d_weight)))) return NUPS_EINVAL;
+    if (!suits(type_bytes(type), d_logits, d_dlogits) || !suits(4, d_choice, d_weight, d_lse, d_dloss, d_dweight) || !suits(8, d_counts, d_tokens)) return NUPS_EINVAL;
     nups_status rc = on_own_device(s);
     if (rc != NUPS_OK || n == 0) return rc;
     RouteGradArgs a = {d_logits, stride, n, experts, top, d_active, renormalize != 0, balance, z, d_choice, d_weight, d_lse, d_counts, d_tokens, d_dloss, d_dweight,

@@ -16,3 +16,48 @@ def test_calls_without_a_store_are_refused():
     assert lib.nups_route_grad(None, None, 0, 4, 1, 4, 1, None, 0, 0.0, 0.0, None, None, None, None, None, None, None, None, 4, None) == binding.EINVAL
     assert lib.nups_orthogonalize_scratch(None, 1, 4, 4, ctypes.byref(size)) == binding.EINVAL and size.value == 77
     assert lib.nups_orthogonalize(None, None, 0, 4, 16, 1, 4, 4, 5, None, 1e-7, 1.0, None, 4, 16, None, 0, None) == binding.EINVAL
+
+
+def test_addresses_that_do_not_suit_their_values_are_refused():
+    # before anything is asked of a device.  The store is made up of ones: its device is none, so that a call which is not refused for its
+    # address ends with another status; nothing here is ever read at an address
+    lib = binding.load()
+    fake = ctypes.create_string_buffer(b"\xff" * 65536, 65536)
+    store, at, much = ctypes.addressof(fake), 1 << 20, 1 << 50
+
+    def goes_on(call):
+        assert call() in (binding.ESTATE, binding.ECUDA)
+
+    def refused(call, *addresses):
+        """One address after the other moved by one byte, and by half a value where its values are larger than that."""
+        goes_on(lambda: call(**{}))
+        for name, size in addresses:
+            for off in {1, size // 2, size - 1}:
+                assert call(**{name: at + off}) == binding.EINVAL, (name, off)
+            goes_on(lambda: call(**{name: at + size}))
+            goes_on(lambda: call(**{name: None})) if name in optional else None
+
+    optional = {"w", "b", "mean", "rstd", "rows", "dw", "db", "dloss", "dweight", "lse", "prob", "loss"}
+    for x_type, size in ((0, 4), (1, 8), (2, 2), (3, 2)):
+        for w_type, w_size in ((x_type, size),) + (((0, 4),) if size == 2 else ()):
+            s_size = 8 if x_type == 1 else 4
+            refused(lambda x=at, y=at, w=at, b=at, mean=at, rstd=at: lib.nups_layer_norm(store, x, x_type, 9, 5, 9, w, b, w_type, 1e-5, y, x_type, 9, mean, rstd, None),
+                    ("x", size), ("y", size), ("w", w_size), ("b", w_size), ("mean", s_size), ("rstd", s_size))
+            optional -= {"mean", "rstd"}                    # the backward pass needs them
+            refused(lambda x=at, dy=at, w=at, mean=at, rstd=at, dx=at, dw=at, db=at: lib.nups_layer_norm_grad(
+                store, x, x_type, 9, dy, x_type, 9, 5, 9, mean, rstd, w, w_type, dx, 9, dw, db, at, much, None),
+                    ("x", size), ("dy", size), ("w", w_size), ("mean", s_size), ("rstd", s_size), ("dx", size), ("dw", w_size), ("db", w_size))
+            optional |= {"mean", "rstd"}
+        if x_type != 1:
+            refused(lambda g=at, out=at: lib.nups_orthogonalize(store, g, x_type, 9, 45, 2, 5, 9, 5, (ctypes.c_float * 3)(1.5, -0.5, 0), 1e-7, 1.0, out, 9, 45, None, 0, None),
+                    ("g", size), ("out", size))
+            refused(lambda x=at, choice=at, weight=at, lse=at, counts=at, tokens=at, prob=at, loss=at: lib.nups_route(
+                store, x, x_type, 9, 5, 9, 2, None, 0, 0.0, 0.0, choice, weight, lse, counts, tokens, prob, loss, at, much, None),
+                    ("x", size), ("choice", 4), ("weight", 4), ("lse", 4), ("counts", 8), ("tokens", 8), ("prob", 4), ("loss", 4))
+            optional -= {"lse"}
+            refused(lambda x=at, choice=at, weight=at, lse=at, counts=at, tokens=at, dloss=at, dweight=at, d=at: lib.nups_route_grad(
+                store, x, x_type, 9, 5, 9, 2, None, 0, 0.0, 0.0, choice, weight, lse, counts, tokens, dloss, dweight, d, 9, None),
+                    ("x", size), ("choice", 4), ("weight", 4), ("lse", 4), ("counts", 8), ("tokens", 8), ("dloss", 4), ("dweight", 4), ("d", size))
+            optional |= {"lse"}
+    refused(lambda keys=at, w=at, b=at, y=at, rows=at, mean=at, rstd=at: lib.nups_pull_norm(store, keys, 5, w, b, 1e-5, y, 0, rows, mean, rstd, None),
+            ("keys", 4), ("w", 4), ("b", 4), ("y", 16), ("rows", 16), ("mean", 4), ("rstd", 4))
