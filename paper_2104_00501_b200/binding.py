@@ -528,10 +528,12 @@ class Store:
             pdw, pdb = dweight.data_ptr(), dbias.data_ptr()
         size = self._scratch_bytes("nups_layer_norm_grad_scratch", n, length, x_type)
         scratch = _scratch_alloc(size, stream) if size else None
-        rc = self._l.nups_layer_norm_grad(self._s, px, x_type, xs, pdy, _type(dy), dys, n, length, pm, pr, pw, TYPES.get(dtype, -1), pdx, dxs, pdw, pdb,
-                                          scratch, size, stream)
-        if scratch:
-            _scratch_free(scratch)
+        try:
+            rc = self._l.nups_layer_norm_grad(self._s, px, x_type, xs, pdy, _type(dy), dys, n, length, pm, pr, pw, TYPES.get(dtype, -1), pdx, dxs, pdw, pdb,
+                                              scratch, size, stream)
+        finally:                                            # also where an argument is of a type that ctypes does not take
+            if scratch:
+                _scratch_free(scratch)
         if rc:
             self._chk(rc, w)
         return dx, dweight, dbias
@@ -563,10 +565,12 @@ class Store:
             pp, pl, pe = prob.data_ptr(), loss.data_ptr(), lse.data_ptr()
         size, stream = self._scratch_bytes("nups_route_scratch", n, experts), _current_stream(self._index)
         scratch = _scratch_alloc(size, stream) if size else None
-        rc = self._l.nups_route(self._s, p, kind, stride, n, experts, top, pa, renormalize, balance, z, choice.data_ptr(), weight.data_ptr(), pe,
-                                counts.data_ptr(), tokens.data_ptr(), pp, pl, scratch, size, stream)
-        if scratch:
-            _scratch_free(scratch)
+        try:
+            rc = self._l.nups_route(self._s, p, kind, stride, n, experts, top, pa, renormalize, balance, z, choice.data_ptr(), weight.data_ptr(), pe,
+                                    counts.data_ptr(), tokens.data_ptr(), pp, pl, scratch, size, stream)
+        finally:
+            if scratch:
+                _scratch_free(scratch)
         if rc:
             self._chk(rc, w)
         return Routing(choice, weight, counts, tokens, prob, loss, lse, active, renormalize, balance, z)
@@ -628,10 +632,12 @@ class Store:
         (pg, gs, gb), (po, os_, ob) = places
         stream, kind = _current_stream(self._index), _type(update)
         scratch = _scratch_alloc(size, stream) if size else None
-        rc = self._l.nups_orthogonalize(self._s, pg, kind, gs, gb, batch, rows, cols, steps, (C.c_float * 3)(*coefficients), eps, scale, po, os_, ob,
-                                        scratch, size, stream)
-        if scratch:
-            _scratch_free(scratch)
+        try:
+            rc = self._l.nups_orthogonalize(self._s, pg, kind, gs, gb, batch, rows, cols, steps, (C.c_float * 3)(*coefficients), eps, scale, po, os_, ob,
+                                            scratch, size, stream)
+        finally:
+            if scratch:
+                _scratch_free(scratch)
         if rc:
             self._chk(rc, w)
         return out

@@ -1,6 +1,9 @@
 """Argument checks of the operators on model tensors that need no device: a call without a store is refused before anything else."""
 import ctypes
 
+import pytest
+import torch
+
 from paper_2104_00501_b200 import binding
 
 
@@ -61,3 +64,60 @@ def test_addresses_that_do_not_suit_their_values_are_refused():
             optional |= {"lse"}
     refused(lambda keys=at, w=at, b=at, y=at, rows=at, mean=at, rstd=at: lib.nups_pull_norm(store, keys, 5, w, b, 1e-5, y, 0, rows, mean, rstd, None),
             ("keys", 4), ("w", 4), ("b", 4), ("y", 16), ("rows", 16), ("mean", 4), ("rstd", 4))
+
+
+# ------------------------------------------------------------------------------------------------
+# the binding's own work, on host tensors: a store whose library takes down the calls
+# ------------------------------------------------------------------------------------------------
+class Calls:
+    """Stands for the library: *_scratch calls name 4096 bytes, the others are converted as ctypes would and taken down."""
+
+    def __init__(self):
+        self.made, self.types = [], binding.load()
+
+    def __getattr__(self, name):
+        types = getattr(self.types, name).argtypes
+
+        def call(*args):
+            assert len(args) == len(types)
+            if name.endswith("_scratch"):
+                args[-1]._obj.value = 4096
+            else:
+                for kind, value in zip(types, args):
+                    kind.from_param(value)
+                self.made.append((name, args))
+            return 0
+        return call
+
+
+@pytest.fixture
+def host(monkeypatch):
+    """(store on host tensors, its calls, sizes of the scratch that is held)."""
+    held = {}
+
+    def alloc(size, stream):
+        at = 1 << 20 | len(held) << 12
+        held[at] = size
+        return at
+
+    monkeypatch.setattr(binding, "_current_device", lambda: -1)
+    monkeypatch.setattr(binding, "_current_stream", lambda index: 0)
+    monkeypatch.setattr(binding, "_scratch_alloc", alloc)
+    monkeypatch.setattr(binding, "_scratch_free", held.pop)
+    s = object.__new__(binding.Store)
+    s._l, s._s, s._index, s._scratch_sizes, s.device, s.dtype, s.L = Calls(), None, -1, {}, torch.device("cpu"), torch.float32, 8
+    return s, s._l.made, held
+
+
+def test_scratch_is_given_back_whatever_becomes_of_the_call(host):
+    s, made, held = host
+    x, mean = torch.ones(200, 300), torch.ones(200)
+    s.route(x, 2, losses=True)
+    s.layer_norm_grad(x, x, mean, mean)
+    s.orthogonalize(x)
+    assert [name for name, _ in made] == ["nups_route", "nups_layer_norm_grad", "nups_orthogonalize"] and not held
+    for call in (lambda: s.orthogonalize(x, steps=5.0), lambda: s.orthogonalize(x, scale="1"), lambda: s.orthogonalize(x, coefficients=(1, 2, "3")),
+                 lambda: s.route(x, 2, z="0"), lambda: s.route(x, 2, renormalize=0.5)):
+        with pytest.raises((TypeError, ctypes.ArgumentError)):
+            call()
+        assert not held
