@@ -175,8 +175,10 @@ def _type(t) -> int:
 
 # Scratch of one call from torch's allocator, on the call's stream and (while one is captured) in its graph's pool: given back as
 # soon as the call's work is enqueued, later work of the stream may have it.  A fourth of the host time of a tensor.
-_current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
-_scratch_alloc, _scratch_free = torch._C._cuda_cudaCachingAllocator_raw_alloc, torch._C._cuda_cudaCachingAllocator_raw_delete
+# (None on a torch without CUDA, where no store can be made.)
+_current_device, _current_stream, _scratch_alloc, _scratch_free = (
+    getattr(torch._C, name, None)
+    for name in ("_cuda_getDevice", "_cuda_getCurrentRawStream", "_cuda_cudaCachingAllocator_raw_alloc", "_cuda_cudaCachingAllocator_raw_delete"))
 
 
 class Routing(NamedTuple):

@@ -1,5 +1,8 @@
 """Argument checks of the operators on model tensors that need no device: a call without a store is refused before anything else."""
 import ctypes
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -121,3 +124,11 @@ def test_scratch_is_given_back_whatever_becomes_of_the_call(host):
         with pytest.raises((TypeError, ctypes.ArgumentError)):
             call()
         assert not held
+
+
+def test_the_module_can_be_imported_on_a_torch_without_cuda():
+    # such a torch has none of these names; inputs, oracles and checks of arguments still use the module there
+    code = "import torch\nfor name in [n for n in dir(torch._C) if n.startswith('_cuda_')]: delattr(torch._C, name)\nfrom paper_2104_00501_b200 import binding\nassert binding.EXPORTS"
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr
