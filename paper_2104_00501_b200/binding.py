@@ -463,6 +463,8 @@ class Store:
         w = "nups_layer_norm"
         if out is None:
             out = torch.empty_like(x) if out_dtype is None else torch.empty_like(x, dtype=out_dtype)
+        elif out_dtype is not None and out.dtype != out_dtype:
+            raise NupsError(EINVAL, w, f"out is of {out.dtype}, out_dtype {out_dtype}")
         self._on_device(w, x, weight, bias, out)
         px, xs = self._rows(w, x)
         n, length = x.shape

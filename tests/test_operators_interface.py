@@ -132,3 +132,18 @@ def test_the_module_can_be_imported_on_a_torch_without_cuda():
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, r.stderr
+
+
+def refused(call):
+    with pytest.raises(binding.NupsError) as e:
+        call()
+    assert e.value.code == binding.EINVAL
+
+
+def test_an_output_of_another_type_than_the_one_asked_for(host):
+    s, made, _ = host
+    x, out = torch.ones(4, 8), torch.empty(4, 8, dtype=torch.bfloat16)
+    for asked in (torch.float32, torch.float16):
+        refused(lambda: s.layer_norm(x, out=out, out_dtype=asked))
+    assert not made
+    assert s.layer_norm(x, out=out, out_dtype=torch.bfloat16, stats=False) is out and s.layer_norm(x, out=out, stats=False) is out and len(made) == 2
