@@ -428,6 +428,8 @@ class Store:
         shape = t.shape
         if len(shape) != 2 or (n is not None and (shape[0] != n or shape[1] != length)):
             raise NupsError(EINVAL, what, f"expected a matrix{'' if n is None else f' of {n} x {length}'}, got {tuple(shape)}")
+        if shape[1] >> 32:                                  # the interface takes 32 bits and ctypes cuts what does not fit
+            raise NupsError(EINVAL, what, f"rows of {shape[1]} values")
         if t.is_contiguous():
             return t.data_ptr(), shape[1]
         stride, step = t.stride()
@@ -626,6 +628,8 @@ class Store:
         if update.dim() not in (2, 3) or out.shape != update.shape or out.dtype != update.dtype or len(coefficients) != 3:
             raise NupsError(EINVAL, w, "expected a matrix or a batch of them, out of the same shape and type, three coefficients")
         (batch, rows, cols), places = (1,) * (3 - update.dim()) + tuple(update.shape), []
+        if max(batch, rows, cols) >> 32 or not 0 < steps <= 64:             # ctypes would cut what does not fit 32 bits
+            raise NupsError(EINVAL, w, f"{batch} matrices of {rows} x {cols}, {steps} steps")
         for t in (update, out):
             if cols > 1 and t.stride(-1) != 1:
                 raise NupsError(EINVAL, w, "the values of a row must be contiguous")

@@ -147,3 +147,18 @@ def test_an_output_of_another_type_than_the_one_asked_for(host):
         refused(lambda: s.layer_norm(x, out=out, out_dtype=asked))
     assert not made
     assert s.layer_norm(x, out=out, out_dtype=torch.bfloat16, stats=False) is out and s.layer_norm(x, out=out, stats=False) is out and len(made) == 2
+
+
+def test_sizes_beyond_32_bits_are_not_cut(host):
+    # 2^32 + 4 would arrive as 4.  Tensors without memory: the calls are refused before they ask for an address
+    s, made, _ = host
+    far = torch.empty((1, 2 ** 32 + 4), dtype=torch.bfloat16, device="meta")
+    stat = torch.ones(1)
+    refused(lambda: s.layer_norm(far))
+    refused(lambda: s.layer_norm_grad(far, far, stat, stat))
+    refused(lambda: s.route(far, 2))
+    for shape in ((2 ** 32 + 4, 1), (1, 2 ** 32 + 4), (2 ** 32 + 4, 1, 1)):
+        refused(lambda: s.orthogonalize(torch.empty(shape, dtype=torch.bfloat16, device="meta")))
+    for steps in (2 ** 32 + 5, 5 - 2 ** 32, -1, 0, 65):
+        refused(lambda: s.orthogonalize(torch.ones(4, 4), steps=steps))
+    assert not made
