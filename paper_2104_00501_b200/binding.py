@@ -593,9 +593,9 @@ class Store:
         p, stride = self._rows(w, logits)
         n, experts = logits.shape
         po, os_ = self._rows(w, out, n, experts)
-        top, pdw = r.choice.shape[1], None
-        if out.dtype != logits.dtype or r.choice.shape[0] != n or r.lse.shape[0] != n or r.counts.shape[0] != experts:
+        if out.dtype != logits.dtype or r.choice.dim() != 2 or r.choice.shape[0] != n or r.lse.shape != (n,) or r.counts.shape != (experts,):
             raise NupsError(EINVAL, w, "out must have the logits' type, and the routing must be of these logits")
+        top, pdw = r.choice.shape[1], None
         # a caller may have put other tensors in their place (sums over processes)
         here = self._index
         if r.counts.dtype != torch.int64 or r.tokens.dtype != torch.int64 or r.tokens.numel() != 1 or not r.counts.is_contiguous() or \

@@ -162,3 +162,15 @@ def test_sizes_beyond_32_bits_are_not_cut(host):
     for steps in (2 ** 32 + 5, 5 - 2 ** 32, -1, 0, 65):
         refused(lambda: s.orthogonalize(torch.ones(4, 4), steps=steps))
     assert not made
+
+
+def test_routings_of_other_shapes(host):
+    s, made, _ = host
+    x = torch.ones(6, 4)
+    r = s.route(x, 2, balance=1.0)
+    s.route_grad(x, r)
+    calls = len(made)
+    for other in (dict(choice=r.choice[:, 0].contiguous()), dict(choice=r.choice.view(6, 2, 1), weight=r.weight.view(6, 2, 1)), dict(lse=torch.ones(6, 2)),
+                  dict(lse=torch.ones(())), dict(counts=torch.ones(4, 2, dtype=torch.int64)), dict(counts=torch.ones((), dtype=torch.int64))):
+        refused(lambda: s.route_grad(x, r._replace(**other)))
+    assert len(made) == calls
