@@ -647,7 +647,11 @@ extern "C" nups_status nups_pull_norm(nups_store* s, const uint32_t* d_keys, uin
     NormArgs a = {s->val, s->value_len, d_y, s->value_len, d_weight, d_bias, d_mean, d_rstd, n, s->value_len, y_type, type, 0, eps, d_keys, d_rows, s->st};
     a.w_vec = params_vec(a, type, type == NUPS_F64 ? 2 : 4);
     const View v = nups_view(s);
-    return type == NUPS_F64 ? launch_norm<double, 2, true>(s, a, v, (cudaStream_t)stream) : launch_norm<float, 4, true>(s, a, v, (cudaStream_t)stream);
+    const cudaStream_t st = (cudaStream_t)stream;
+    nups_time_begin(s, st, NUPS_TIMED_PULL);
+    rc = type == NUPS_F64 ? launch_norm<double, 2, true>(s, a, v, st) : launch_norm<float, 4, true>(s, a, v, st);
+    nups_time_end(s, st);
+    return rc;
 }
 
 // ---------------------------------------------------------------------------------------------

@@ -472,3 +472,19 @@ def test_very_long_rows_of_equal_values(store, dtype):
     dy = torch.full_like(x, 0.1)
     dy[1, ::2] = -0.2
     check_grad(x, dy, mean, rstd, None, store.layer_norm_grad(x, dy, mean, rstd, need_params=False))
+
+
+def test_the_time_of_a_normalised_pull_is_a_pulls():
+    s = binding.Store(1000, 64)
+    keys = dev_keys(np.arange(500))
+    s.kernel_timing(True)
+    s.pull(keys)
+    y = s.pull_norm(keys)[0]
+    s.pull_norm(keys, rows=True)
+    s.kernel_timing(False)
+    s.pull_norm(keys)
+    times = s.kernel_times()
+    assert times["pull"][0] > 0 and [n for _, n in times.values()] == [3, 0, 0, 0, 0]
+    s.kernel_timing(True)
+    assert torch.equal(s.pull_norm(keys)[0], y)
+    s.close()
