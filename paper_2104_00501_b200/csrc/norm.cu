@@ -674,10 +674,29 @@ struct GradArgs {
     DevStat* st;
 };
 
-// One pass: a team holds x and dy of ROWS rows in registers and, over all of its rows, its columns' shares of dweight and dbias
+// Rows that are added one after the other before the sums go to (and are added in) the block's part of scratch: the rounding of a
+// sum over n rows grows with this number and with n / (blocks * SUM_RUN), not with n / blocks (3M rows of 300 equal values: 1.5e-6 of the
+// sum, 4.9e-5 with one run per block).  With 64 rows 60,000 rows of 1000 bf16 took 89 us, with 128 they take 79.
+constexpr uint32_t SUM_RUN = 128;
+// N sums into a block's part of scratch: stored the first time, added after that.  N loads in flight, not all of a thread's, so that
+// this takes no registers from the loop.
+template <int N, class A> __device__ __forceinline__ void put_sums(A* to, A* sums, bool before)
+{
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        to[j] = before ? to[j] + sums[j] : sums[j];
+        sums[j] = 0;
+    }
+    asm volatile("" ::: "memory");
+}
+
+// One pass: a team holds x and dy of ROWS rows in registers and, over SUM_RUN of its rows, its columns' shares of dweight and dbias
 // (SHARED: in shared memory, where 64 registers a thread leave no room; each thread has its own columns there).
+// Short rows of floats by 16 bytes: three blocks per multiprocessor, as many as grad_blocks gives (the compiler would take 96
+// registers, for two).  The others as the compiler sees fit.
+constexpr int grad_min_blocks(int tpr, int vec, int ept, size_t d) { return tpr <= 32 && vec == 4 && (ept == 4 || d == 2) ? 3 : 0; }
 template <class X, class D, int VEC, int TPR, int CH, int ROWS>
-__global__ void __launch_bounds__(team_block(TPR)) norm_grad_kernel(GradArgs a)
+__global__ void __launch_bounds__(team_block(TPR), grad_min_blocks(TPR, VEC, CH * VEC, sizeof(D))) norm_grad_kernel(GradArgs a)
 {
     typedef typename Acc<X>::type A;
     constexpr int BLOCK = team_block(TPR), TEAMS = BLOCK / TPR, WARPS = BLOCK / 32, EPT = CH * VEC;
@@ -698,157 +717,165 @@ __global__ void __launch_bounds__(team_block(TPR)) norm_grad_kernel(GradArgs a)
             else dw[c][j] = db[c][j] = 0;
         }
     const A inv_len = (A)1 / (A)a.len;
-    int turn = 0;
-    for (uint64_t base = (uint64_t)blockIdx.x * (TEAMS * ROWS); base < a.n; base += (uint64_t)gridDim.x * (TEAMS * ROWS), ++turn) {
-        Pack<X, VEC> x[ROWS][CH];
-        Pack<D, VEC> dy[ROWS][CH];
-        A mean[ROWS], rstd[ROWS], s1[ROWS], s2[ROWS];
-#pragma unroll
-        for (int k = 0; k < ROWS; ++k) {
-            const uint64_t row = base + k * TEAMS + team;
-            const bool in = row < a.n;
-            mean[k] = in ? ((const A*)a.mean)[row] : (A)0;
-            rstd[k] = in ? ((const A*)a.rstd)[row] : (A)0;
+    A* const out = (A*)a.part + (uint64_t)blockIdx.x * 2 * a.len;
+    bool before = false;
+    auto put_down = [&] {                                   // the whole block
+        if (TPR > 32) {
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 const uint32_t at = value_at<TPR, VEC>(c, t);
-                if (in && at < a.len) {
-                    x[k][c] = load_pack<X, VEC>((const X*)a.x + row * a.xs + at);
-                    dy[k][c] = load_pack<D, VEC>((const D*)a.dy + row * a.dys + at);
-                } else {
-                    x[k][c] = Pack<X, VEC>{};
-                    dy[k][c] = Pack<D, VEC>{};
+                if (at < a.len) {
+                    put_sums<VEC>(out + at, SHARED ? sum_w + at : dw[c], before);
+                    put_sums<VEC>(out + a.len + at, SHARED ? sum_b + at : db[c], before);
+                }
+            }
+        } else {
+            // teams of a warp by shuffles, warps through shared memory; first dweight, then dbias
+            A* mine = shared + (threadIdx.x >> 5) * TPR * EPT;
+#pragma unroll
+            for (int which = 0; which < 2; ++which) {
+                __syncthreads();
+#pragma unroll
+                for (int c = 0; c < CH; ++c)
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) {
+                        A p = which ? db[c][j] : dw[c][j];
+#pragma unroll
+                        for (int o = TPR; o < 32; o <<= 1) p += __shfl_xor_sync(0xFFFFFFFFu, p, o);
+                        if ((threadIdx.x & 31) < TPR) mine[value_at<TPR, VEC>(c, t) + j] = p;
+                        if (which) db[c][j] = 0;
+                        else dw[c][j] = 0;
+                    }
+                __syncthreads();
+                for (uint32_t i = threadIdx.x; i < a.len; i += BLOCK) {
+                    A sum = 0;
+#pragma unroll
+                    for (int k = 0; k < WARPS; ++k) sum += shared[k * TPR * EPT + i];
+                    out[which * a.len + i] = before ? out[which * a.len + i] + sum : sum;
                 }
             }
         }
-        A a1[ROWS][2], a2[ROWS][2];
+        before = true;
+    };
+    int turn = 0;
+    uint64_t base = (uint64_t)blockIdx.x * (TEAMS * ROWS);
+    do {
+        for (int end = turn + SUM_RUN / ROWS; turn < end && base < a.n; base += (uint64_t)gridDim.x * (TEAMS * ROWS), ++turn) {
+            Pack<X, VEC> x[ROWS][CH];
+            Pack<D, VEC> dy[ROWS][CH];
+            A mean[ROWS], rstd[ROWS], s1[ROWS], s2[ROWS];
 #pragma unroll
-        for (int k = 0; k < ROWS; ++k) a1[k][0] = a1[k][1] = a2[k][0] = a2[k][1] = 0;
+            for (int k = 0; k < ROWS; ++k) {
+                const uint64_t row = base + k * TEAMS + team;
+                const bool in = row < a.n;
+                mean[k] = in ? ((const A*)a.mean)[row] : (A)0;
+                rstd[k] = in ? ((const A*)a.rstd)[row] : (A)0;
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const uint32_t at = value_at<TPR, VEC>(c, t);
-            if (at < a.len) {
-                A wc[1][VEC], dwc[VEC], dbc[VEC];
-                if (SHARED) {
-                    load_params_at<X, A, VEC>(a.w, a.w_type, a.w_vec, at, (A)1, wc);
-#pragma unroll
-                    for (int j = 0; j < VEC; ++j) { dwc[j] = sum_w[at + j]; dbc[j] = sum_b[at + j]; }
-                }
-                // rows that are not there have dy = 0 and rstd = 0: they add nothing
-#pragma unroll
-                for (int k = 0; k < ROWS; ++k) {
-                    const A minus = -mean[k];
-                    A h[VEC], d[VEC];
-                    unpack<A>(x[k][c], h);
-                    unpack<A>(dy[k][c], d);
-                    run_add<VEC, true>(h, h, &minus);
-                    run_scale<VEC>(h, h, rstd[k]);
-                    run_fma<VEC, false, false, false>(SHARED ? dwc : dw[c], d, h, SHARED ? dwc : dw[c]);
-                    run_add<VEC, false>(SHARED ? dbc : db[c], SHARED ? dbc : db[c], d);
-                    run_mul<VEC>(d, d, SHARED ? wc[0] : w[c]);
-                    sum_run<VEC>(a1[k], d);
-                    sum_run_of_products<VEC>(a2[k], d, h);
-                }
-                if (SHARED)
-#pragma unroll
-                    for (int j = 0; j < VEC; ++j) { sum_w[at + j] = dwc[j]; sum_b[at + j] = dbc[j]; }
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < ROWS; ++k) { s1[k] = a1[k][0] + a1[k][1]; s2[k] = a2[k][0] + a2[k][1]; }
-        if (!a.dx) continue;                                // the same for the whole grid
-#pragma unroll
-        for (int k = 0; k < ROWS; ++k) {
-            s1[k] = team_sum<(TPR < 32 ? TPR : 32)>(s1[k]);
-            s2[k] = team_sum<(TPR < 32 ? TPR : 32)>(s2[k]);
-        }
-        if (TPR > 32) {
-            A* st = shared + (turn & 1) * 2 * ROWS * WARPS;
-            const int lane = t & 31;
-            if (lane == 0)
-#pragma unroll
-                for (int k = 0; k < ROWS; ++k) { st[k * WARPS + (t >> 5)] = s1[k]; st[(ROWS + k) * WARPS + (t >> 5)] = s2[k]; }
-            __syncthreads();
-            // lanes [i WARPS, (i + 1) WARPS) take sum i of the 2 ROWS, 32 / WARPS sums at a time
-            constexpr int AT_ONCE = 32 / WARPS < 2 * ROWS ? 32 / WARPS : 2 * ROWS;
-#pragma unroll
-            for (int i0 = 0; i0 < 2 * ROWS; i0 += AT_ONCE) {
-                const A sum = team_sum<WARPS>(st[(i0 + (lane / WARPS) % AT_ONCE) * WARPS + lane % WARPS]);
-#pragma unroll
-                for (int i = 0; i < AT_ONCE; ++i) {
-                    const A r = __shfl_sync(0xFFFFFFFFu, sum, i * WARPS);
-                    if (i0 + i < ROWS) s1[i0 + i] = r;
-                    else s2[i0 + i - ROWS] = r;
+                for (int c = 0; c < CH; ++c) {
+                    const uint32_t at = value_at<TPR, VEC>(c, t);
+                    if (in && at < a.len) {
+                        x[k][c] = load_pack<X, VEC>((const X*)a.x + row * a.xs + at);
+                        dy[k][c] = load_pack<D, VEC>((const D*)a.dy + row * a.dys + at);
+                    } else {
+                        x[k][c] = Pack<X, VEC>{};
+                        dy[k][c] = Pack<D, VEC>{};
+                    }
                 }
             }
-        }
+            A a1[ROWS][2], a2[ROWS][2];
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const uint32_t at = value_at<TPR, VEC>(c, t);
-            if (at < a.len) {
-                A wc[1][VEC];
-                if (SHARED) load_params_at<X, A, VEC>(a.w, a.w_type, a.w_vec, at, (A)1, wc);
+            for (int k = 0; k < ROWS; ++k) a1[k][0] = a1[k][1] = a2[k][0] = a2[k][1] = 0;
 #pragma unroll
-                for (int k = 0; k < ROWS; ++k) {
-                    const uint64_t row = base + k * TEAMS + team;
-                    // rstd (g - mean(g) - h mean(g h)), the two means with the factor rstd already
-                    const A minus = -mean[k], m1 = -s1[k] * inv_len * rstd[k], m2 = -s2[k] * inv_len * rstd[k];
-                    A h[VEC], d[VEC];
-                    unpack<A>(x[k][c], h);
-                    unpack<A>(dy[k][c], d);
-                    run_add<VEC, true>(h, h, &minus);
-                    run_scale<VEC>(h, h, rstd[k]);
-                    run_mul<VEC>(d, d, SHARED ? wc[0] : w[c]);
-                    run_fma<VEC, false, true, true>(h, h, &m2, &m1);
-                    run_fma<VEC, false, true, false>(d, d, &rstd[k], h);
-                    if (row < a.n) store_values<X, VEC>((X*)a.dx + row * a.dxs + at, d);
+            for (int c = 0; c < CH; ++c) {
+                const uint32_t at = value_at<TPR, VEC>(c, t);
+                if (at < a.len) {
+                    A wc[1][VEC], dwc[VEC], dbc[VEC];
+                    if (SHARED) {
+                        load_params_at<X, A, VEC>(a.w, a.w_type, a.w_vec, at, (A)1, wc);
+#pragma unroll
+                        for (int j = 0; j < VEC; ++j) { dwc[j] = sum_w[at + j]; dbc[j] = sum_b[at + j]; }
+                    }
+                    // rows that are not there have dy = 0 and rstd = 0: they add nothing
+#pragma unroll
+                    for (int k = 0; k < ROWS; ++k) {
+                        const A minus = -mean[k];
+                        A h[VEC], d[VEC];
+                        unpack<A>(x[k][c], h);
+                        unpack<A>(dy[k][c], d);
+                        run_add<VEC, true>(h, h, &minus);
+                        run_scale<VEC>(h, h, rstd[k]);
+                        run_fma<VEC, false, false, false>(SHARED ? dwc : dw[c], d, h, SHARED ? dwc : dw[c]);
+                        run_add<VEC, false>(SHARED ? dbc : db[c], SHARED ? dbc : db[c], d);
+                        run_mul<VEC>(d, d, SHARED ? wc[0] : w[c]);
+                        sum_run<VEC>(a1[k], d);
+                        sum_run_of_products<VEC>(a2[k], d, h);
+                    }
+                    if (SHARED)
+#pragma unroll
+                        for (int j = 0; j < VEC; ++j) { sum_w[at + j] = dwc[j]; sum_b[at + j] = dbc[j]; }
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k) { s1[k] = a1[k][0] + a1[k][1]; s2[k] = a2[k][0] + a2[k][1]; }
+            if (!a.dx) continue;                                // the same for the whole grid
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k) {
+                s1[k] = team_sum<(TPR < 32 ? TPR : 32)>(s1[k]);
+                s2[k] = team_sum<(TPR < 32 ? TPR : 32)>(s2[k]);
+            }
+            if (TPR > 32) {
+                A* st = shared + (turn & 1) * 2 * ROWS * WARPS;
+                const int lane = t & 31;
+                if (lane == 0)
+#pragma unroll
+                    for (int k = 0; k < ROWS; ++k) { st[k * WARPS + (t >> 5)] = s1[k]; st[(ROWS + k) * WARPS + (t >> 5)] = s2[k]; }
+                __syncthreads();
+                // lanes [i WARPS, (i + 1) WARPS) take sum i of the 2 ROWS, 32 / WARPS sums at a time
+                constexpr int AT_ONCE = 32 / WARPS < 2 * ROWS ? 32 / WARPS : 2 * ROWS;
+#pragma unroll
+                for (int i0 = 0; i0 < 2 * ROWS; i0 += AT_ONCE) {
+                    const A sum = team_sum<WARPS>(st[(i0 + (lane / WARPS) % AT_ONCE) * WARPS + lane % WARPS]);
+#pragma unroll
+                    for (int i = 0; i < AT_ONCE; ++i) {
+                        const A r = __shfl_sync(0xFFFFFFFFu, sum, i * WARPS);
+                        if (i0 + i < ROWS) s1[i0 + i] = r;
+                        else s2[i0 + i - ROWS] = r;
+                    }
+                }
+            }
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const uint32_t at = value_at<TPR, VEC>(c, t);
+                if (at < a.len) {
+                    A wc[1][VEC];
+                    if (SHARED) load_params_at<X, A, VEC>(a.w, a.w_type, a.w_vec, at, (A)1, wc);
+#pragma unroll
+                    for (int k = 0; k < ROWS; ++k) {
+                        const uint64_t row = base + k * TEAMS + team;
+                        // rstd (g - mean(g) - h mean(g h)), the two means with the factor rstd already
+                        const A minus = -mean[k], m1 = -s1[k] * inv_len * rstd[k], m2 = -s2[k] * inv_len * rstd[k];
+                        A h[VEC], d[VEC];
+                        unpack<A>(x[k][c], h);
+                        unpack<A>(dy[k][c], d);
+                        run_add<VEC, true>(h, h, &minus);
+                        run_scale<VEC>(h, h, rstd[k]);
+                        run_mul<VEC>(d, d, SHARED ? wc[0] : w[c]);
+                        run_fma<VEC, false, true, true>(h, h, &m2, &m1);
+                        run_fma<VEC, false, true, false>(d, d, &rstd[k], h);
+                        if (row < a.n) store_values<X, VEC>((X*)a.dx + row * a.dxs + at, d);
+                    }
                 }
             }
         }
-    }
-    if (!a.part) return;
-    A* out = (A*)a.part + (uint64_t)blockIdx.x * 2 * a.len;
-    if (TPR > 32) {
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const uint32_t at = value_at<TPR, VEC>(c, t);
-            if (at < a.len)
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) {
-                    out[at + j] = SHARED ? sum_w[at + j] : dw[c][j];
-                    out[a.len + at + j] = SHARED ? sum_b[at + j] : db[c][j];
-                }
-        }
-    } else {
-        // teams of a warp by shuffles, warps through shared memory; first dweight, then dbias
-        A* mine = shared + (threadIdx.x >> 5) * TPR * EPT;
-#pragma unroll
-        for (int which = 0; which < 2; ++which) {
-            __syncthreads();
-#pragma unroll
-            for (int c = 0; c < CH; ++c)
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) {
-                    A p = which ? db[c][j] : dw[c][j];
-#pragma unroll
-                    for (int o = TPR; o < 32; o <<= 1) p += __shfl_xor_sync(0xFFFFFFFFu, p, o);
-                    if ((threadIdx.x & 31) < TPR) mine[value_at<TPR, VEC>(c, t) + j] = p;
-                }
-            __syncthreads();
-            for (uint32_t i = threadIdx.x; i < a.len; i += BLOCK) {
-                A sum = 0;
-#pragma unroll
-                for (int k = 0; k < WARPS; ++k) sum += shared[k * TPR * EPT + i];
-                out[which * a.len + i] = sum;
-            }
-        }
-    }
+        if (a.part) put_down();
+    } while (base < a.n);
 }
 
 // Rows above 1 KB: x and dy come through a ring in shared memory, as in norm_ring_kernel, and are read there twice.
-// (16,384 rows of 4096 bf16: 90 us with the rows in registers.)
+// (16,384 rows of 4096 bf16: 90 us with the rows in registers.)  As many blocks per multiprocessor as grad_blocks gives: with the compiler's
+// own choice of registers the same rows take 87 us instead of 84, 60,000 of 1000 bf16 81 instead of 79.
 template <class X, class D, int TPR, int CH, int ROWS, int STAGES>
-__global__ void __launch_bounds__(TPR) norm_grad_ring_kernel(GradArgs a)
+__global__ void __launch_bounds__(TPR, 512 / TPR) norm_grad_ring_kernel(GradArgs a)
 {
     typedef typename Acc<X>::type A;
     constexpr int VEC = 16 / sizeof(X), WARPS = TPR / 32;
@@ -885,101 +912,109 @@ __global__ void __launch_bounds__(TPR) norm_grad_ring_kernel(GradArgs a)
 #pragma unroll
         for (int j = 0; j < VEC; ++j) dw[c][j] = db[c][j] = 0;
     const A inv_len = (A)1 / (A)a.len;
-    __syncthreads();                                        // the barriers are there
-    uint32_t i = 0;
-    bool ok = true;
-    for (uint64_t base = first; base < a.n; base += step, ++i) {
-        const uint32_t s = i % STAGES;
-        const X* x = (const X*)(ring + s * stage_bytes);
-        const D* dy = (const D*)(ring + s * stage_bytes + ROWS * x_bytes);
-        A mean[ROWS], rstd[ROWS], s1[ROWS], s2[ROWS];
-#pragma unroll
-        for (int k = 0; k < ROWS; ++k) {
-            mean[k] = base + k < a.n ? ((const A*)a.mean)[base + k] : (A)0;
-            rstd[k] = base + k < a.n ? ((const A*)a.rstd)[base + k] : (A)0;
-        }
-        ok = mbar_wait(bar(s), (i / STAGES) & 1);
-        auto hat = [&](int k, uint32_t at, A* h, A* d) {
-            const A minus = -mean[k];
-            unpack<A>(load_pack<X, VEC>(x + k * a.len + at), h);
-            unpack<A>(load_pack<D, VEC>(dy + k * a.len + at), d);
-            run_add<VEC, true>(h, h, &minus);
-            run_scale<VEC>(h, h, rstd[k]);
-        };
-#pragma unroll
-        for (int k = 0; k < ROWS; ++k) {
-            A a1[2] = {0, 0}, a2[2] = {0, 0};
-            if (base + k < a.n)                             // the same for the whole block
-#pragma unroll
-                for (int c = 0; c < CH; ++c) {
-                    const uint32_t at = value_at<TPR, VEC>(c, t);
-                    if (at < a.len) {
-                        A h[VEC], d[VEC];
-                        hat(k, at, h, d);
-                        run_fma<VEC, false, false, false>(dw[c], d, h, dw[c]);
-                        run_add<VEC, false>(db[c], db[c], d);
-                        run_mul<VEC>(d, d, w[c]);
-                        sum_run<VEC>(a1, d);
-                        sum_run_of_products<VEC>(a2, d, h);
-                    }
-                }
-            s1[k] = a1[0] + a1[1];
-            s2[k] = a2[0] + a2[1];
-        }
-#pragma unroll
-        for (int k = 0; k < ROWS; ++k) {
-            s1[k] = team_sum<32>(s1[k]);
-            s2[k] = team_sum<32>(s2[k]);
-        }
-        A* st = shared + (i & 1) * 2 * ROWS * WARPS;
-        const int lane = t & 31;
-        if (lane == 0)
-#pragma unroll
-            for (int k = 0; k < ROWS; ++k) { st[k * WARPS + (t >> 5)] = s1[k]; st[(ROWS + k) * WARPS + (t >> 5)] = s2[k]; }
-        if (__syncthreads_or(!ok)) { ok = false; break; }
-        if (t == 0) issue(i + STAGES - 1);                  // every thread is done with the group before this one
-        if (!a.dx) continue;
-        constexpr int AT_ONCE = 32 / WARPS < 2 * ROWS ? 32 / WARPS : 2 * ROWS;
-#pragma unroll
-        for (int i0 = 0; i0 < 2 * ROWS; i0 += AT_ONCE) {
-            const A sum = team_sum<WARPS>(st[(i0 + (lane / WARPS) % AT_ONCE) * WARPS + lane % WARPS]);
-#pragma unroll
-            for (int q = 0; q < AT_ONCE; ++q) {
-                const A r = __shfl_sync(0xFFFFFFFFu, sum, q * WARPS);
-                if (i0 + q < ROWS) s1[i0 + q] = r;
-                else s2[i0 + q - ROWS] = r;
-            }
-        }
+    A* const out = (A*)a.part + (uint64_t)blockIdx.x * 2 * a.len;
+    bool before = false;
+    auto put_down = [&] {                                   // as in norm_grad_kernel
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const uint32_t at = value_at<TPR, VEC>(c, t);
-            if (at < a.len)
-#pragma unroll
-                for (int k = 0; k < ROWS; ++k) {
-                    const A m1 = -s1[k] * inv_len * rstd[k], m2 = -s2[k] * inv_len * rstd[k];
-                    A h[VEC], d[VEC];
-                    hat(k, at, h, d);
-                    run_mul<VEC>(d, d, w[c]);
-                    run_fma<VEC, false, true, true>(h, h, &m2, &m1);
-                    run_fma<VEC, false, true, false>(d, d, &rstd[k], h);
-                    if (base + k < a.n) store_values<X, VEC>((X*)a.dx + (base + k) * a.dxs + at, d);
-                }
+            if (at < a.len) {
+                put_sums<VEC>(out + at, dw[c], before);
+                put_sums<VEC>(out + a.len + at, db[c], before);
+            }
         }
-    }
+        before = true;
+    };
+    __syncthreads();                                        // the barriers are there
+    uint32_t i = 0;
+    bool ok = true;
+    uint64_t base = first;
+    do {
+        for (uint32_t end = i + SUM_RUN / ROWS; i < end && base < a.n; base += step, ++i) {
+            const uint32_t s = i % STAGES;
+            const X* x = (const X*)(ring + s * stage_bytes);
+            const D* dy = (const D*)(ring + s * stage_bytes + ROWS * x_bytes);
+            A mean[ROWS], rstd[ROWS], s1[ROWS], s2[ROWS];
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k) {
+                mean[k] = base + k < a.n ? ((const A*)a.mean)[base + k] : (A)0;
+                rstd[k] = base + k < a.n ? ((const A*)a.rstd)[base + k] : (A)0;
+            }
+            ok = mbar_wait(bar(s), (i / STAGES) & 1);
+            auto hat = [&](int k, uint32_t at, A* h, A* d) {
+                const A minus = -mean[k];
+                unpack<A>(load_pack<X, VEC>(x + k * a.len + at), h);
+                unpack<A>(load_pack<D, VEC>(dy + k * a.len + at), d);
+                run_add<VEC, true>(h, h, &minus);
+                run_scale<VEC>(h, h, rstd[k]);
+            };
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k) {
+                A a1[2] = {0, 0}, a2[2] = {0, 0};
+                if (base + k < a.n)                             // the same for the whole block
+#pragma unroll
+                    for (int c = 0; c < CH; ++c) {
+                        const uint32_t at = value_at<TPR, VEC>(c, t);
+                        if (at < a.len) {
+                            A h[VEC], d[VEC];
+                            hat(k, at, h, d);
+                            run_fma<VEC, false, false, false>(dw[c], d, h, dw[c]);
+                            run_add<VEC, false>(db[c], db[c], d);
+                            run_mul<VEC>(d, d, w[c]);
+                            sum_run<VEC>(a1, d);
+                            sum_run_of_products<VEC>(a2, d, h);
+                        }
+                    }
+                s1[k] = a1[0] + a1[1];
+                s2[k] = a2[0] + a2[1];
+            }
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k) {
+                s1[k] = team_sum<32>(s1[k]);
+                s2[k] = team_sum<32>(s2[k]);
+            }
+            A* st = shared + (i & 1) * 2 * ROWS * WARPS;
+            const int lane = t & 31;
+            if (lane == 0)
+#pragma unroll
+                for (int k = 0; k < ROWS; ++k) { st[k * WARPS + (t >> 5)] = s1[k]; st[(ROWS + k) * WARPS + (t >> 5)] = s2[k]; }
+            if (__syncthreads_or(!ok)) { ok = false; break; }
+            if (t == 0) issue(i + STAGES - 1);                  // every thread is done with the group before this one
+            if (!a.dx) continue;
+            constexpr int AT_ONCE = 32 / WARPS < 2 * ROWS ? 32 / WARPS : 2 * ROWS;
+#pragma unroll
+            for (int i0 = 0; i0 < 2 * ROWS; i0 += AT_ONCE) {
+                const A sum = team_sum<WARPS>(st[(i0 + (lane / WARPS) % AT_ONCE) * WARPS + lane % WARPS]);
+#pragma unroll
+                for (int q = 0; q < AT_ONCE; ++q) {
+                    const A r = __shfl_sync(0xFFFFFFFFu, sum, q * WARPS);
+                    if (i0 + q < ROWS) s1[i0 + q] = r;
+                    else s2[i0 + q - ROWS] = r;
+                }
+            }
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const uint32_t at = value_at<TPR, VEC>(c, t);
+                if (at < a.len)
+#pragma unroll
+                    for (int k = 0; k < ROWS; ++k) {
+                        const A m1 = -s1[k] * inv_len * rstd[k], m2 = -s2[k] * inv_len * rstd[k];
+                        A h[VEC], d[VEC];
+                        hat(k, at, h, d);
+                        run_mul<VEC>(d, d, w[c]);
+                        run_fma<VEC, false, true, true>(h, h, &m2, &m1);
+                        run_fma<VEC, false, true, false>(d, d, &rstd[k], h);
+                        if (base + k < a.n) store_values<X, VEC>((X*)a.dx + (base + k) * a.dxs + at, d);
+                    }
+            }
+        }
+        if (a.part) put_down();
+    } while (ok && base < a.n);
     if (!ok) {                                              // a copy did not come: say so, and leave none in flight
         atomicCAS(&a.st->status, 0, NUPS_ETIMEOUT);
         if (t == 0)
             for (uint32_t k = i + 1; k < i + STAGES - 1; ++k)
                 if (first + k * step < a.n) mbar_wait(bar(k % STAGES), (k / STAGES) & 1);
-    }
-    if (!a.part) return;
-    A* out = (A*)a.part + (uint64_t)blockIdx.x * 2 * a.len;
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-        const uint32_t at = value_at<TPR, VEC>(c, t);
-        if (at < a.len)
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) { out[at + j] = dw[c][j]; out[a.len + at + j] = db[c][j]; }
     }
 }
 
@@ -1024,7 +1059,16 @@ __global__ void __launch_bounds__(256) norm_grad_apply_kernel(GradArgs a, const 
     load_params_at<X, A, VEC>(a.w, a.w_type, a.w_vec, at, (A)1, w);
 #pragma unroll
     for (int j = 0; j < VEC; ++j) dw[j] = db[j] = 0;
-    for (uint64_t row = blockIdx.y; row < a.n; row += gridDim.y) {
+    A* const out = (A*)a.part + (uint64_t)blockIdx.y * 2 * a.len + at;
+    bool before = false;
+    auto put_down = [&] {                                   // as in norm_grad_kernel
+        put_sums<VEC>(out, dw, before);
+        put_sums<VEC>(out + a.len, db, before);
+        before = true;
+    };
+    uint32_t run = 0;
+    for (uint64_t row = blockIdx.y; row < a.n; row += gridDim.y, ++run) {
+        if (a.part && run == SUM_RUN) { put_down(); run = 0; }
         const A mean = ((const A*)a.mean)[row], rstd = ((const A*)a.rstd)[row];
         A x[VEC], g[VEC], d[VEC];
         unpack<A>(load_pack<X, VEC>((const X*)a.x + row * a.xs + at), x);
@@ -1039,11 +1083,7 @@ __global__ void __launch_bounds__(256) norm_grad_apply_kernel(GradArgs a, const 
         }
         if (a.dx) store_values<X, VEC>((X*)a.dx + row * a.dxs + at, d);
     }
-    if (a.part) {
-        A* out = (A*)a.part + (uint64_t)blockIdx.y * 2 * a.len + at;
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) { out[j] = dw[j]; out[a.len + j] = db[j]; }
-    }
+    if (a.part) put_down();
 }
 
 // dweight and dbias: the blocks' sums, added in a fixed order.  32 columns and 32 runs of blocks per block of threads.

@@ -84,3 +84,17 @@ def test_orthogonalized_update_far_into_a_tensor():
     wide = torch.as_strided(g, (2, 300, 300), (4_500_000_000, 300, 1))  # a batch stride beyond 32 bits
     wide[1] = g[-1]
     assert torch.equal(s.orthogonalize(wide)[1], last) and torch.equal(s.orthogonalize(wide)[0], s.orthogonalize(g[0]))
+
+
+@pytest.mark.parametrize("n,length", [(3_000_000, 300), (4_000_000, 128)])
+def test_sums_over_millions_of_rows(n, length):
+    # equal values, whose roundings all go one way.  A team adds at most 128 rows one after the other, a block at most 9 such runs, 8 warps
+    # and 32 lanes, the last kernel 19 blocks and 32 runs of them: at most 220 roundings with those of the terms
+    room(10)
+    s = binding.Store(64, 64)
+    x = torch.full((n, length), 0.1, device="cuda")
+    mean, rstd = torch.full((n,), -0.2, device="cuda"), torch.full((n,), 1.1, device="cuda")
+    _, dw, db = s.layer_norm_grad(x, x, mean, rstd, torch.ones(length, device="cuda"), need_dx=False)
+    v = x[0, 0].double()
+    for got, term in ((db, v), (dw, v * (v - mean[0].double()) * rstd[0].double())):
+        assert ((got.double() - n * term).abs() <= 220 * 2.0 ** -24 * n * term).all()
