@@ -362,9 +362,9 @@ nups_status nups_get_clip_stats(nups_store* store, double* h_sum, uint64_t* h_co
  *   - x_type and the like are NUPS_F32, NUPS_F64, NUPS_F16 or NUPS_BF16.
  *   - Row i of a matrix argument starts `stride` VALUES after row i - 1 and its
  *     values are contiguous; rows of an output must not overlap.  Any alignment
- *     that suits the type is allowed, 16-byte aligned rows are fastest.  An output
- *     overlaps an input only where a call names it (the same rows in the same
- *     places), and no other output.
+ *     that suits the type is allowed (another address is NUPS_EINVAL), 16-byte
+ *     aligned rows are fastest.  An output overlaps an input only where a call
+ *     names it (the same rows in the same places), and no other output.
  *   - Sums and statistics are held in fp32, or fp64 for fp64 values.
  *   - d_scratch is the caller's device memory, 256-byte aligned, of at least the
  *     bytes that the *_scratch call names for the same sizes; it needs no
@@ -379,10 +379,11 @@ enum { NUPS_F32 = 0, NUPS_F64 = 1, NUPS_F16 = 2, NUPS_BF16 = 3 };
 /* Layer norm of the n rows of x, `len` values each (1 <= len < 2^28):
  *   mean = sum x / len, rstd = 1 / sqrt(sum (x - mean)^2 / len + eps),
  *   y = (x - mean) rstd weight + bias.
- * y has x's type; for fp32 x it may also be fp16 or bf16.  weight and bias (either
- * may be NULL: 1 and 0) are of w_type: x's type or fp32 (fp64 x: fp64).  mean and
- * rstd (NULL: not wanted) are fp32 (fp64 x: fp64), one value per row.  eps > 0.
- * y may be x (same type and stride).                                           */
+ * The difference is formed first: a row of equal values gives bias wherever its
+ * mean is exact.  y has x's type; for fp32 x it may also be fp16 or bf16.  weight
+ * and bias (either may be NULL: 1 and 0) are of w_type: x's type or fp32 (fp64 x:
+ * fp64).  mean and rstd (NULL: not wanted) are fp32 (fp64 x: fp64), one value per
+ * row.  eps > 0.  y may be x (same type and stride).                            */
 nups_status nups_layer_norm(nups_store* store, const void* d_x, int x_type, uint64_t x_stride, uint64_t n, uint32_t len,
                             const void* d_weight, const void* d_bias, int w_type, double eps, void* d_y, int y_type,
                             uint64_t y_stride, void* d_mean, void* d_rstd, void* stream);
@@ -425,10 +426,13 @@ nups_status nups_layer_norm_grad_scratch(nups_store* store, uint64_t n, uint32_t
  * logits hold; its choices are -1 and its other results 0.  So are those of an item
  * whose logits are all -infinity.  A logit of -infinity is not chosen (-1 and 0
  * where fewer than `top` are left), and neither is NaN.  NaN and +infinity make the
- * item's p, and with it prob and the losses, NaN.  T = 0: prob and loss are 0.  Choices are keys as the store's
- * calls take them where experts are its first keys.  type is NUPS_F32, NUPS_F16 or
- * NUPS_BF16; 1 <= experts <= NUPS_ROUTE_MAX_EXPERTS; top <= experts,
- * NUPS_ROUTE_MAX_TOP.                                                           */
+ * item's p, and with it prob and the losses, NaN.  T = 0: prob and loss are 0.
+ * Exponentials are the device's fast ones, about the item's largest logit (here and
+ * in the gradient): p of an expert d below it is off by up to 2^-23 (2 + 1.2 d) of
+ * itself and by the sum's error, whatever the size of the logits.  Choices are keys
+ * as the store's calls take them where experts are its first keys; -1 is a key out
+ * of range there.  type is NUPS_F32, NUPS_F16 or NUPS_BF16;
+ * 1 <= experts <= NUPS_ROUTE_MAX_EXPERTS; top <= experts, NUPS_ROUTE_MAX_TOP.     */
 #define NUPS_ROUTE_MAX_EXPERTS 1024
 #define NUPS_ROUTE_MAX_TOP 32
 nups_status nups_route(nups_store* store, const void* d_logits, int type, uint64_t stride, uint64_t n, uint32_t experts, uint32_t top,
@@ -439,9 +443,10 @@ nups_status nups_route_scratch(nups_store* store, uint64_t n, uint32_t experts, 
 
 /* The gradient of the logits from that of the loss (d_dloss, one float; NULL: 1)
  * and that of the weights (d_dweight [n][top]; NULL: 0).  Choices and counts are
- * constants.  d_choice, d_weight, d_lse, d_counts and d_tokens are what nups_route gave
- * for the same arguments (the first two are needed with d_dweight).  d_dlogits has the logits' type; items that took no part get 0.
- * d_dlogits may be d_logits (same stride).                                      */
+ * constants.  d_choice, d_weight, d_lse, d_counts and d_tokens are what nups_route
+ * gave for the same arguments (the first two are needed with d_dweight).
+ * d_dlogits has the logits' type; items that took no part get 0.  d_dlogits may be
+ * d_logits (same stride).                                                       */
 nups_status nups_route_grad(nups_store* store, const void* d_logits, int type, uint64_t stride, uint64_t n, uint32_t experts, uint32_t top,
                             const uint8_t* d_active, int renormalize, float balance, float z, const int32_t* d_choice,
                             const float* d_weight, const float* d_lse, const uint64_t* d_counts, const uint64_t* d_tokens, const float* d_dloss,
@@ -464,9 +469,9 @@ nups_status nups_route_grad(nups_store* store, const void* d_logits, int type, u
  * fp16 values that hold 22 bits of each number, with fp32 sums.  A matrix of
  * zeros gives zeros; NaN or infinity in a matrix makes that matrix NaN.
  * h_coefficients = {a, b, c}.  1 <= steps <= NUPS_ORTHOGONALIZE_MAX_STEPS, eps > 0,
- * 1 <= rows, cols <= NUPS_ORTHOGONALIZE_MAX_SIZE, batch <= 65535.  NUPS_EINVAL also when
- * the iteration with these coefficients carries a singular value from [0, 1]
- * above 2.5, or a factor a + b s^2 + c s^4 above 7.5: its products would leave the
+ * 1 <= rows, cols <= NUPS_ORTHOGONALIZE_MAX_SIZE, batch <= 65535.  NUPS_EINVAL also
+ * when the iteration with these coefficients carries any singular value from [0, 1]
+ * above 2.5, or its factor |a + b s^2 + c s^4| above 7.5: products would leave the
  * range of the fp16 pairs.                                                      */
 #define NUPS_ORTHOGONALIZE_MAX_STEPS 64
 #define NUPS_ORTHOGONALIZE_MAX_SIZE 65536
@@ -490,10 +495,11 @@ nups_status nups_status_check(nups_store* store, void* stream);
 nups_status nups_get_stats(nups_store* store, uint64_t* h_out, void* stream);
 
 /* Timing aid for benchmarks.  While enabled, the library records a pair of CUDA
- * events on the call's stream around the main kernel of nups_pull*, nups_push*
- * (fast mode) and nups_step_* (the row gather, the scatter-add, the fused step
- * kernel).  nups_kernel_timing only switches the recording on or off (no
- * synchronisation; pairs already recorded stay until they are queried), so a
+ * events on the call's stream around the main kernel of nups_pull* (nups_pull_norm
+ * among them), nups_push* (fast mode) and nups_step_* (the row gather, the
+ * scatter-add, the fused step kernel).  nups_kernel_timing only switches the
+ * recording on or off (no synchronisation; pairs already recorded stay until they
+ * are queried), so a
  * caller can time some repetitions of a loop and leave the others undisturbed:
  * an event between two kernels keeps the second from starting while the first
  * drains.  nups_kernel_time synchronises the stream, adds up the elapsed

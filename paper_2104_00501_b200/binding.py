@@ -401,8 +401,9 @@ class Store:
         return torch.as_tensor(_Raw(), device=self.device).clone()
 
     # -- operators on model tensors -----------------------------------------------------
-    # All tensors are on the store's device, which is the current one; the calls run on its current stream.  Small calls are
-    # bound by the host, so the checks are written for the case that passes.
+    # All tensors are on the store's device, which is the current one; the calls run on its current stream.  They take no part in
+    # torch's differentiation: what they give for a tensor that requires a gradient requires none, the backward passes are calls of
+    # their own (layer_norm_grad, route_grad).  Small calls are bound by the host, so the checks are written for the case that passes.
     def _on_device(self, what, *tensors):
         here = self._index
         if _current_device() != here:
@@ -461,7 +462,7 @@ class Store:
         return self._vector(what, bias, length)
 
     def layer_norm(self, x, weight=None, bias=None, eps=1e-5, out_dtype=None, stats=True, out=None):
-        """(y, mean, rstd) of the rows of x [n, len]; stats=False: y alone.  out may be x itself."""
+        """(y, mean, rstd) of the rows of x [n, len]; stats=False: y alone.  out may be x itself; out_dtype, where both are given, is its type."""
         w = "nups_layer_norm"
         if out is None:
             out = torch.empty_like(x) if out_dtype is None else torch.empty_like(x, dtype=out_dtype)

@@ -547,9 +547,9 @@ nups_status launch_norm(nups_store* s, const NormArgs& a, const View& v, cudaStr
         nups_launch_dependent(norm_kernel<X, VEC, TPR_, CH_, ROWS_, KEYED>, grid, team_block(TPR_), 0, st, a, v);                          \
     }
     if constexpr (VEC * sizeof(X) == 16) {
-        // short rows: several teams to a warp with a few chunks per lane, one row each (1M pulled rows of 128 floats: 205 us with
-        // 8 lanes of 4 chunks, 209 with 16 of 2, two rows each, 278 with 32 of 1, four rows each;
-        // the lookups' running ahead took the first to 197)
+        // short rows: several teams to a warp with a few chunks per lane, one row each (1M pulled rows of 128 floats, the kernel by
+        // itself: 205 us with 8 lanes of 4 chunks, 209 with 16 of 2, two rows each, 278 with 32 of 1, four rows each; the lookups'
+        // running ahead took the first to 197.  Among other calls it takes 208.)
         if (chunks <= 4) NUPS_NORM(4, 1, 2)
         else if (chunks <= 8) NUPS_NORM(4, 2, 1)
         else if (chunks <= 16) NUPS_NORM((VEC <= 4 ? 4 : 8), (VEC <= 4 ? 4 : 2), 1)

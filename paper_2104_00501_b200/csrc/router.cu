@@ -188,6 +188,8 @@ template <int EPT> __device__ __forceinline__ void exponentials(const float* x, 
     for (int i = 0; i < EPT; ++i) ex[i] = exp2_fast(ex[i]);
 }
 
+// Blocks per multiprocessor as in route_blocks.  With 16 or 32 logits per lane that leaves too few registers: by 16-byte loads, 12 to 44
+// bytes a thread are spilled with 32 16-bit logits, 28 to 180 with 16 float ones.
 template <class X, int VEC, int TPR, int EPT, int KEPT>
 __global__ void __launch_bounds__(ROUTE_BLOCK, EPT <= 8 ? 4 : EPT <= 16 ? 3 : 2) route_kernel(RouteArgs a)
 {
