@@ -392,7 +392,8 @@ nups_status nups_layer_norm(nups_store* store, const void* d_x, int x_type, uint
  * of what nups_pull gives for d_keys[i] (replica rows, access counts and keys out
  * of range as there).  weight and bias have the store's value type, y_type as
  * above.  d_rows (NULL: not wanted) receives the pulled rows themselves, which the
- * backward pass reads.  d_y and d_rows are [n][value_len], 16-byte aligned.      */
+ * backward pass reads.  d_y and d_rows are [n][value_len], 16-byte aligned;
+ * value_len < 2^28 as above.                                                    */
 nups_status nups_pull_norm(nups_store* store, const uint32_t* d_keys, uint64_t n, const void* d_weight, const void* d_bias,
                            double eps, void* d_y, int y_type, void* d_rows, void* d_mean, void* d_rstd, void* stream);
 

@@ -644,6 +644,7 @@ extern "C" nups_status nups_pull_norm(nups_store* s, const uint32_t* d_keys, uin
     if (!suits(16, d_y, d_rows) || !suits(4, d_keys) || !suits(type_bytes(type), d_weight, d_bias, d_mean, d_rstd)) return NUPS_EINVAL;
     nups_status rc = on_own_device(s);
     if (rc != NUPS_OK || n == 0) return rc;
+    if (s->value_len >= (1u << 28)) return NUPS_EINVAL;     // positions within a row are 32 bits, and run some thousand past its end
     NormArgs a = {s->val, s->value_len, d_y, s->value_len, d_weight, d_bias, d_mean, d_rstd, n, s->value_len, y_type, type, 0, eps, d_keys, d_rows, s->st};
     a.w_vec = params_vec(a, type, type == NUPS_F64 ? 2 : 4);
     const View v = nups_view(s);

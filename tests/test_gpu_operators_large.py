@@ -98,3 +98,24 @@ def test_sums_over_millions_of_rows(n, length):
     v = x[0, 0].double()
     for got, term in ((db, v), (dw, v * (v - mean[0].double()) * rstd[0].double())):
         assert ((got.double() - n * term).abs() <= 220 * 2.0 ** -24 * n * term).all()
+
+
+def test_normalised_pull_of_the_longest_rows():
+    # rows of 2^28 values and more are refused, as layer_norm refuses them: positions within a row are held in 32 bits
+    room(12)
+    s = binding.Store(1, 1 << 28)
+    with pytest.raises(binding.NupsError) as e:
+        s.pull_norm(dev_keys([0]))
+    assert e.value.code == binding.EINVAL
+    s.close()
+    s = binding.Store(1, (1 << 28) - 4)
+    s.init_uniform(0, 1, 0.5)
+    y, mean, rstd, rows = s.pull_norm(dev_keys([0]), rows=True)
+    want = s.layer_norm(rows)
+    assert torch.equal(y, want[0]) and torch.equal(mean, want[1]) and torch.equal(rstd, want[2])
+    # the sums' own rounding is 2^-53 a step: what is left is the roundings of a difference, its square, the mean and rstd
+    x = rows.double()
+    m = x.mean()
+    v = ((x - m) ** 2).mean()
+    assert abs(mean.item() - m) <= 2.0 ** -24 * abs(m) + 1e-9 and abs(rstd.item() * torch.sqrt(v + 1e-5).item() - 1) <= 16 * 2.0 ** -24
+    s.close()
